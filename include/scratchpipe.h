@@ -352,13 +352,128 @@ sp_status sp_debug_plan(sp_handle h, int64_t ticket, sp_plan_dump *out);
 void sp_destroy(sp_handle h);
 
 /* Text of the last error on this context (or of the last failed sp_create
- * when h is NULL).  Valid until the next call on the context. */
+ * or call without a context when h is NULL, by this thread).  Valid until the
+ * next call on the context. */
 const char *sp_last_error(sp_handle h);
 
 /* Pinned, device-mapped host memory for host tables (hipHostMalloc with the
  * mapped and portable flags; exact size).  *ptr is set on SP_OK. */
 sp_status sp_host_alloc(size_t bytes, void **ptr);
 void sp_host_free(void *ptr);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Operators on token tables and 8-bit rows, on device memory.
+ *
+ * A table of rows is trained (sp_lookup, sp_lookup_grad, sp_dropout), then kept
+ * in 8 bits, read back (sp_cache_write, sp_cache_read) and scored against
+ * (sp_product).  These calls take no context.  They enqueue kernels on `stream`
+ * of the current device, allocate nothing, keep nothing, wait for nothing (so
+ * they can be captured into a graph), and may be used from several threads.
+ *
+ *  - A matrix is a pointer, its element type and `ld`, the elements from the
+ *    start of one row to the next (at least its columns); the elements of a row
+ *    follow one another.  Rows may start at any multiple of the element's size.
+ *  - At most 2^31 - 1 rows of anything, 2^20 columns (sp_dropout 2^30).
+ *  - Results do not depend on the order in which the device runs blocks.  Sums
+ *    are held in fp32 (sp_product: in 32-bit integers) and rounded once.
+ *  - Outputs overlap no input, except where a call says so.
+ *  - Errors: SP_ERR_INVALID_ARG (nothing was enqueued), SP_ERR_HIP (a launch
+ *    failed); text from sp_last_error(NULL).
+ */
+#define SP_F32 0
+#define SP_BF16 1
+#define SP_F16 2
+#define SP_I32 3
+#define SP_I64 4
+#define SP_I8 5
+#define SP_F8 6 /* 1 sign, 4 exponent, 3 mantissa bits, no infinities, largest 448 */
+
+/*
+ * out[i][:] = scale * table[tokens[i]][:], i < n, with dropout of probability p
+ * (0: none) as sp_dropout's, row i being row i of its generator.  tokens: SP_I32 or
+ * SP_I64; a token outside 0 .. rows-1 (padding) gives a row of zeros.  table and
+ * out: SP_F32, SP_BF16 or SP_F16 each.
+ */
+sp_status sp_lookup(const void *tokens, int32_t token_type, int64_t n, const void *table,
+                    int32_t table_type, int64_t rows, int64_t dim, int64_t table_ld, float scale,
+                    float p, uint64_t seed, uint64_t offset, void *out, int32_t out_type,
+                    int64_t out_ld, void *stream);
+
+/*
+ * The gradient of sp_lookup to its table: out[r][:] = scale * the sum of the
+ * gradients of the positions with token r, as the same p, seed and offset let
+ * them through, in a fixed order.  Rows without a token become zeros; with
+ * accumulate != 0 the sums are added to out, and rows without a token are neither
+ * read nor written.  grad [n][dim] and out [rows][dim]: SP_F32, SP_BF16 or SP_F16
+ * each.  Gradients of tokens that are no rows are not read.
+ * workspace: device memory of at least the bytes that sp_lookup_grad_workspace
+ * gives for n, rows and dim (0 for few tokens), 16-byte aligned, in use until the
+ * call's work is done; its content means nothing before and after.
+ */
+sp_status sp_lookup_grad_workspace(int64_t n, int64_t rows, int64_t dim, int64_t *bytes);
+sp_status sp_lookup_grad(const void *tokens, int32_t token_type, int64_t n, const void *grad,
+                         int32_t grad_type, int64_t dim, int64_t grad_ld, float scale, float p,
+                         uint64_t seed, uint64_t offset, void *out, int32_t out_type, int64_t rows,
+                         int64_t out_ld, int32_t accumulate, void *workspace,
+                         int64_t workspace_bytes, void *stream);
+
+/*
+ * out = [residual +] x / (1 - p) where kept, [residual + ] 0 where dropped.  The mask
+ * is drawn from seed, offset and the element's row and column and stored nowhere:
+ * the gradient to x is the same call on the output's gradient without a residual
+ * (the residual's is the output's gradient itself).  Give every use its own offset.
+ * The generator is Philox 4x32-10 with counter (column / 8, row, offset low, offset
+ * high) and key (seed low, seed high); its four words are 16 bits for each of 8
+ * columns, the low half of a word first; a column is dropped where they are below
+ * 65536 p, rounded to an integer.  1 - p is taken from that integer.
+ * x, residual (may be NULL) and out have one type: SP_F32, SP_BF16 or SP_F16.
+ * out may be x or residual itself (same pointer and ld).
+ */
+sp_status sp_dropout(const void *x, int32_t type, int64_t n, int64_t dim, int64_t x_ld,
+                     const void *residual, int64_t residual_ld, float p, uint64_t seed,
+                     uint64_t offset, void *out, int64_t out_ld, void *stream);
+
+/*
+ * A cache of rows in 8 bits: q [slots][dim] (SP_I8 or SP_F8) and fp32 scales
+ * [slots][dim / group], a scale for each `group` columns of a slot (group: dim, or a
+ * multiple of 8 that divides dim).
+ *
+ * sp_cache_write quantises row i of x (SP_F32, SP_BF16 or SP_F16) into slot index[i]
+ * (SP_I32 or SP_I64; NULL: slot i).  scale = the group's largest magnitude / 127
+ * (SP_I8) or / 448 (SP_F8), byte = x / scale rounded to nearest, ties to even.  A
+ * group with an infinity or NaN reads back as NaN; one whose scale is below the
+ * smallest normal fp32 number is held as zeros.  Rows whose index is no slot are not
+ * read.  The slots of one call are distinct: which of two rows, or what mixture
+ * of them, one slot gets is not defined.
+ *
+ * sp_cache_read gives out[i][:] = byte * scale of slot index[i], zeros where the index
+ * is no slot.
+ */
+sp_status sp_cache_write(const void *x, int32_t type, int64_t n, int64_t dim, int64_t x_ld,
+                         const void *index, int32_t index_type, int64_t group, void *q,
+                         int32_t kind, int64_t slots, int64_t q_ld, float *scales,
+                         int64_t scales_ld, void *stream);
+sp_status sp_cache_read(const void *q, int32_t kind, int64_t slots, int64_t dim, int64_t q_ld,
+                        const float *scales, int64_t scales_ld, int64_t group, const void *index,
+                        int32_t index_type, int64_t n, void *out, int32_t out_type, int64_t out_ld,
+                        void *stream);
+
+/*
+ * out[i][j] = x_scales[i] * w_scales[j] * sum over c < k of x[i][c] * w[j][c], i < m, j < n,
+ * of 8-bit integers (-128 .. 127), the sum exact (k: 1 .. 131071).  With x from
+ * sp_cache_write (group = dim) the scales are those of its tokens, with w a cache
+ * they are those of its rows.  out: SP_F32, SP_BF16 or SP_F16.  Fastest where x and w
+ * start at, and their strides are, multiples of 16; their rows are then read in whole
+ * aligned 16-byte pieces (what lies beyond k in the last one counts nothing).
+ * workspace: as for sp_lookup_grad, of the bytes that sp_product_workspace gives for
+ * m, n and k.
+ */
+sp_status sp_product_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes);
+sp_status sp_product(const int8_t *x, const float *x_scales, int64_t m, int64_t x_ld,
+                     const int8_t *w, const float *w_scales, int64_t n, int64_t w_ld, int64_t k,
+                     void *out, int32_t out_type, int64_t out_ld, void *workspace,
+                     int64_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libscratchpipe.so")
-SOURCES = ["k_ingest.hip", "k_plan.hip", "k_train.hip", "capi.cpp"]
+SOURCES = ["k_ingest.hip", "k_plan.hip", "k_train.hip", "k_tokens.hip", "k_tokengrad.hip",
+           "k_cache.hip", "k_product.hip", "capi.cpp", "rowapi.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -598,6 +598,16 @@ static sp_status fail(sp_ctx *h, sp_status code, const char *fmt, ...)
     return code;
 }
 
+// Errors of the calls that take no context: sp_last_error(NULL) reports them.
+sp_status sp::set_error(sp_status code, const char *text)
+{
+    try {
+        return fail(nullptr, code, "%s", text);
+    } catch (...) {  // no memory for the text
+        return code;
+    }
+}
+
 #define HIPCHK(h, call)                                                                        \
     do {                                                                                       \
         hipError_t _e = (call);                                                                \

@@ -1,0 +1,685 @@
+// Gradient of a token lookup, summed by sorted tokens into a dense table gradient.
+//
+//   out[r] (+)= factor * sum over the positions i with token r of keep(i) * grad[i]
+//
+// in ascending order of position within fixed pieces, so a result never depends on the
+// order in which blocks run, with fp32 sums rounded once when they are stored.  Rows
+// without a token become zeros (or stay, where the sums are added).  Three ways to
+// bring a token's positions together, by their number:
+//   up to DIRECT_MAX   every position's block looks at all tokens itself: one launch
+//   up to RANK_MAX     every position counts the entries before its own: its place
+//   above              radix sort, stable, of (token, position)
+// After the last two, k_grad_sum walks over the sorted entries in equal pieces,
+// whatever the lengths of the runs, and k_grad_join adds up runs that were cut.
+#include "sp_rows.h"
+
+namespace sp {
+
+constexpr int64_t DIRECT_MAX = 512;
+constexpr int64_t RANK_MAX = 8192;
+constexpr int SLAB = WAVE * OCT;  // columns of one wave
+
+// A sorted entry: token (rows for one that is no row) above its position.
+__device__ __forceinline__ uint32_t key_of(uint64_t e) { return (uint32_t)(e >> 32); }
+
+template <typename IX>
+__device__ __forceinline__ uint32_t key_at(const IX *tokens, int64_t i, int64_t rows)
+{
+    const int64_t t = (int64_t)tokens[i];
+    return t >= 0 && t < rows ? (uint32_t)t : (uint32_t)rows;
+}
+
+__device__ __forceinline__ void zero_oct(float (&v)[OCT])
+{
+#pragma unroll
+    for (int k = 0; k < OCT; ++k) v[k] = 0.f;
+}
+
+// The octet of one position, where the position is live, as dropout lets it through.
+template <typename TI>
+__device__ __forceinline__ void grad_oct(const GradArgs &a, int64_t pos, int32_t oct, bool live,
+                                         float (&v)[OCT])
+{
+    zero_oct(v);
+    if (!live) return;
+    load_oct((const TI *)a.grad + pos * a.grad_ld + oct * OCT, oct_valid(a.dim, oct), v);
+    if (a.drop.drop) {  // the same for the whole launch
+        const uint32_t keep = keep_oct(a.drop, (uint32_t)oct, (uint32_t)pos);
+#pragma unroll
+        for (int k = 0; k < OCT; ++k) v[k] = keep >> k & 1u ? v[k] : 0.f;
+    }
+}
+
+// A finished sum goes to its row of the table gradient.
+template <typename TO>
+__device__ __forceinline__ void put_oct(const GradArgs &a, int64_t row, int32_t oct,
+                                        const float (&v)[OCT])
+{
+    TO *p = (TO *)a.out + row * a.out_ld + oct * OCT;
+    const int valid = oct_valid(a.dim, oct);
+    float w[OCT];
+    if (a.add) {
+        load_oct(p, valid, w);
+#pragma unroll
+        for (int k = 0; k < OCT; ++k) w[k] += a.factor * v[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < OCT; ++k) w[k] = a.factor * v[k];
+    }
+    store_oct(p, valid, w);
+}
+
+// ---------------------------------------------------------------- few positions
+
+// Block b < sums: one position and slab of columns.  Every wave looks for the
+// position's token among all tokens, 64 at a time; the token's first position adds up
+// its rows (each wave those of every fourth group of 64 positions, joined in LDS).  The
+// other blocks write zeros to their rows without a token.
+constexpr int FILL_UNITS = 2048;  // octets that one block of a fill looks after
+template <typename TI, typename TO, typename IX>
+__global__ void __launch_bounds__(BLOCK) k_grad_direct(GradArgs a, int32_t slabs, int64_t sums,
+                                                       Split fill)
+{
+    __shared__ float part[3][SLAB];
+    __shared__ uint8_t used[FILL_UNITS];
+    const IX *tokens = (const IX *)a.tokens;
+    const int n = (int)a.n;
+    if ((int64_t)blockIdx.x < sums) {
+        const int i = (int)(blockIdx.x / slabs);
+        const int32_t oct = (int32_t)(blockIdx.x % slabs) * WAVE + lane_id();
+        const uint32_t key = key_at(tokens, i, a.rows);
+        if (key == (uint32_t)a.rows) return;
+        uint64_t mine[DIRECT_MAX / WAVE];
+        bool first = true;
+#pragma unroll
+        for (int g = 0; g < (int)(DIRECT_MAX / WAVE); ++g) {
+            const int p = g * WAVE + lane_id();
+            mine[g] = __ballot(p < n && key_at(tokens, p < n ? p : 0, a.rows) == key);
+            if (g < i / WAVE) first = first && mine[g] == 0;
+            if (g == i / WAVE) first = first && (mine[g] & ((1ull << (i % WAVE)) - 1)) == 0;
+        }
+        if (!first) return;  // the whole block
+        const bool on = oct * OCT < a.dim;
+        float acc[OCT];
+        zero_oct(acc);
+#pragma unroll
+        for (int g = 0; g < (int)(DIRECT_MAX / WAVE); ++g) {
+            if (g % 4 != wave_id()) continue;
+            uint64_t m = mine[g];
+            while (m) {
+                float v[4][OCT];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int p = g * WAVE + __ffsll((unsigned long long)m) - 1;
+                    grad_oct<TI>(a, m ? p : 0, oct, on && m != 0, v[k]);
+                    m &= m - 1;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int c = 0; c < OCT; ++c) acc[c] += v[k][c];
+            }
+        }
+        if (wave_id() > 0) {
+#pragma unroll
+            for (int c = 0; c < OCT; ++c) part[wave_id() - 1][c * WAVE + lane_id()] = acc[c];
+        }
+        __syncthreads();
+        if (wave_id() == 0 && on) {
+#pragma unroll
+            for (int w = 0; w < 3; ++w)
+#pragma unroll
+                for (int c = 0; c < OCT; ++c) acc[c] += part[w][c * WAVE + lane_id()];
+            put_oct<TO>(a, key, oct, acc);
+        }
+        return;
+    }
+    const int64_t b = (int64_t)blockIdx.x - sums;
+    const int64_t row0 = b / fill.stretches * fill.rows;
+    for (int u = threadIdx.x; u < FILL_UNITS; u += BLOCK) used[u] = 0;
+    __syncthreads();
+    for (int p = threadIdx.x; p < n; p += BLOCK) {
+        const int64_t r = (int64_t)key_at(tokens, p, a.rows) - row0;
+        if (r >= 0 && r < fill.rows) used[r] = 1;
+    }
+    __syncthreads();
+    float z[OCT];
+    zero_oct(z);
+    for (int u = threadIdx.x; u < FILL_UNITS; u += BLOCK) {
+        int64_t row;
+        int32_t oct;
+        if (split_at(fill, b, u, row, oct) && !used[row - row0])
+            store_oct((TO *)a.out + row * a.out_ld + oct * OCT, oct_valid(a.dim, oct), z);
+    }
+}
+
+// ---------------------------------------------------------------- places by counting
+
+// 64 positions per block, one per lane; 16 waves count over a sixteenth of the keys each.
+constexpr int RANK_NT = 1024;
+template <typename IX>
+__global__ void __launch_bounds__(RANK_NT) k_grad_rank(const IX *tokens, int32_t n, int64_t rows,
+                                                       uint64_t *out)
+{
+    __shared__ uint32_t keys[RANK_MAX];
+    __shared__ uint32_t count[RANK_NT / WAVE][WAVE];
+    for (int i = threadIdx.x; i < n; i += RANK_NT) keys[i] = key_at(tokens, i, rows);
+    __syncthreads();
+    const int i = (int)blockIdx.x * WAVE + lane_id();
+    const uint32_t k = keys[i < n ? i : 0];
+    const int per = (n + RANK_NT / WAVE - 1) / (RANK_NT / WAVE);
+    const int j0 = wave_id() * per, j1 = j0 + per < n ? j0 + per : n;
+    uint32_t c = 0;
+    int j = j0;
+    for (; j < j1 && j < (int)blockIdx.x * WAVE; ++j) c += keys[j] <= k;  // before the block's own
+    for (; j < j1 && j < (int)blockIdx.x * WAVE + WAVE; ++j) c += keys[j] < k || (keys[j] == k && j < i);
+    for (; j < j1; ++j) c += keys[j] < k;
+    count[wave_id()][lane_id()] = c;
+    __syncthreads();
+    if (threadIdx.x < WAVE && i < n) {
+        uint32_t at = 0;
+#pragma unroll
+        for (int w = 0; w < RANK_NT / WAVE; ++w) at += count[w][threadIdx.x];
+        out[at] = (uint64_t)k << 32 | (uint32_t)i;
+    }
+}
+
+// ---------------------------------------------------------------- radix sort
+
+// Stable, least digit first, SORT_TILE entries per block.  Per pass the tiles count
+// their digits (hist[tile][digit]); a tile of the scatter adds up what the digits below
+// its own and the tiles before it hold, by itself while there are few tiles
+// (SELF_TILES), after k_grad_prefix otherwise.
+constexpr int SORT_NT = 512;
+constexpr int SORT_ITEMS = 8;
+constexpr int SORT_TILE = SORT_NT * SORT_ITEMS;
+constexpr int DIGIT_MAX = 9;
+constexpr int BINS_MAX = 1 << DIGIT_MAX;
+constexpr int SELF_TILES = 64;
+static_assert(BINS_MAX <= SORT_NT, "one thread per digit");
+
+struct Digits {
+    int32_t shift, bits;
+};
+
+template <typename IX, bool FIRST>
+__device__ __forceinline__ uint64_t sort_entry(const void *in, int64_t i, int64_t rows)
+{
+    if constexpr (FIRST)
+        return (uint64_t)key_at((const IX *)in, i, rows) << 32 | (uint32_t)i;
+    else
+        return ((const uint64_t *)in)[i];
+}
+
+template <typename IX, bool FIRST>
+__global__ void __launch_bounds__(SORT_NT) k_grad_hist(const void *in, int64_t n, int64_t rows,
+                                                       Digits d, uint32_t *hist)
+{
+    __shared__ uint32_t bin[BINS_MAX];
+    const int t = (int)threadIdx.x;
+    if (t < BINS_MAX) bin[t] = 0;
+    __syncthreads();
+    const int64_t i0 = (int64_t)blockIdx.x * SORT_TILE;
+#pragma unroll
+    for (int k = 0; k < SORT_ITEMS; ++k) {
+        const int64_t i = i0 + k * SORT_NT + t;
+        if (i < n)
+            atomicAdd(&bin[key_of(sort_entry<IX, FIRST>(in, i, rows)) >> d.shift & ((1u << d.bits) - 1)],
+                      1u);
+    }
+    __syncthreads();
+    if (t < 1 << d.bits) hist[(int64_t)blockIdx.x << d.bits | t] = bin[t];
+}
+
+// hist[tile][digit] becomes the entries of that digit in the tiles before; the digits'
+// totals go behind the last tile.
+__global__ void __launch_bounds__(SORT_NT) k_grad_prefix(uint32_t *hist, int64_t tiles, int32_t bits)
+{
+    const int t = (int)threadIdx.x;
+    if (t >= 1 << bits) return;
+    uint32_t sum = 0;
+    int64_t k = 0;
+    for (; k + 8 <= tiles; k += 8) {
+        uint32_t x[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = hist[(k + q) << bits | t];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            hist[(k + q) << bits | t] = sum;
+            sum += x[q];
+        }
+    }
+    for (; k < tiles; ++k) {
+        const uint32_t x = hist[k << bits | t];
+        hist[k << bits | t] = sum;
+        sum += x;
+    }
+    hist[tiles << bits | t] = sum;
+}
+
+template <typename IX, bool FIRST>
+__global__ void __launch_bounds__(SORT_NT) k_grad_scatter(const void *in, int64_t n, int64_t rows,
+                                                          Digits d, const uint32_t *hist,
+                                                          int64_t tiles, bool prefixed,
+                                                          uint64_t *out)
+{
+    constexpr int NW = SORT_NT / WAVE;
+    __shared__ uint32_t cnt[NW][BINS_MAX];
+    __shared__ uint32_t lds[NW];
+    const int t = (int)threadIdx.x, w = wave_id(), lane = lane_id();
+    const int bins = 1 << d.bits;
+    for (int b = lane; b < bins; b += WAVE) cnt[w][b] = 0;
+    // what lies before this tile's entries of digit t
+    uint32_t total = 0, before = 0;
+    if (t < bins) {
+        if (prefixed) {
+            before = hist[(int64_t)blockIdx.x << d.bits | t];
+            total = hist[tiles << d.bits | t];
+        } else {
+            for (int64_t k = 0; k < tiles; k += 8) {
+                uint32_t x[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    x[q] = k + q < tiles ? hist[(k + q) << d.bits | t] : 0u;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    total += x[q];
+                    before += k + q < (int64_t)blockIdx.x ? x[q] : 0u;
+                }
+            }
+        }
+    }
+    // entries, and the place of each among its wave's of the same digit: the waves
+    // take consecutive stretches, the rounds of a wave follow one another
+    const int64_t i0 = (int64_t)blockIdx.x * SORT_TILE + w * (SORT_ITEMS * WAVE);
+    uint64_t e[SORT_ITEMS];
+    uint32_t place[SORT_ITEMS];
+#pragma unroll
+    for (int k = 0; k < SORT_ITEMS; ++k) {
+        const int64_t i = i0 + k * WAVE + lane;
+        e[k] = i < n ? sort_entry<IX, FIRST>(in, i, rows) : 0;
+    }
+    __syncthreads();
+    volatile uint32_t *mine = cnt[w];
+#pragma unroll
+    for (int k = 0; k < SORT_ITEMS; ++k) {
+        const bool on = i0 + k * WAVE + lane < n;
+        const uint32_t dig = key_of(e[k]) >> d.shift & (uint32_t)(bins - 1);
+        uint64_t same = __ballot(on);
+        for (int q = 0; q < d.bits; ++q) {
+            const uint64_t has = __ballot(dig >> q & 1u);
+            same &= dig >> q & 1u ? has : ~has;
+        }
+        const uint32_t base = mine[dig];
+        place[k] = base + (uint32_t)__popcll(same & lanemask_lt());
+        if (on && (same & lanemask_lt()) == 0) mine[dig] = base + (uint32_t)__popcll(same);
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    uint32_t all;
+    const uint32_t digits_below = block_excl_scan_n<SORT_NT>(total, lds, all);
+    if (t < bins) {
+        uint32_t run = digits_below + before;
+#pragma unroll
+        for (int q = 0; q < NW; ++q) {
+            const uint32_t x = cnt[q][t];
+            cnt[q][t] = run;
+            run += x;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SORT_ITEMS; ++k) {
+        if (i0 + k * WAVE + lane < n) {
+            const uint32_t dig = key_of(e[k]) >> d.shift & (uint32_t)(bins - 1);
+            out[cnt[w][dig] + place[k]] = e[k];
+        }
+    }
+}
+
+// ---------------------------------------------------------------- sums
+
+// A team of LPR lanes (an octet each) walks over `per` sorted entries and a slab of
+// columns; a block's teams follow one another.  A run that lies within a team's piece
+// is stored at once.  The others leave their parts in LDS, and the team (or, into the
+// block, the first one) where the run begins adds them up in order; what crosses the
+// block's edges goes to `part`: [block][0] what continues from the block before,
+// [block][1] what begins here and continues.  Blocks after the sums write the zeros:
+// they find their rows' entries by bisection.
+constexpr int SUM_NT = 512;
+constexpr int SUM_AHEAD = 8;
+
+struct SumShape {
+    int32_t per;      // entries per team
+    int32_t slabs;    // of LPR octets
+    int64_t chunks;   // blocks along the entries
+    int64_t part_ld;  // floats of one row of part
+};
+
+// First index in [lo, hi) whose key is at least `key`, else hi.
+__device__ __forceinline__ int64_t first_at_least(const uint64_t *e, int64_t lo, int64_t hi,
+                                                  uint32_t key)
+{
+    while (lo < hi) {
+        const int64_t mid = lo + (hi - lo) / 2;
+        if (key_of(e[mid]) < key) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <typename TI, typename TO, int LPR>
+__global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t *e, SumShape sh,
+                                                     float *part, Split fill)
+{
+    constexpr int TEAMS = SUM_NT / LPR;
+    __shared__ float head[OCT][SUM_NT], tail[OCT][SUM_NT];
+    __shared__ uint8_t through[TEAMS];
+    __shared__ uint8_t used[FILL_UNITS];
+    const int64_t n = a.n, sums = sh.chunks * sh.slabs;
+    if ((int64_t)blockIdx.x < sums) {
+        const int64_t chunk = (int64_t)blockIdx.x / sh.slabs;
+        const int team = (int)threadIdx.x / LPR;
+        const int32_t oct = (int32_t)(blockIdx.x % sh.slabs) * LPR + (int)threadIdx.x % LPR;
+        const bool on = oct * OCT < a.dim;
+        const int64_t c0 = chunk * sh.per * TEAMS;
+        int64_t p0 = c0 + (int64_t)team * sh.per, p1 = p0 + sh.per;
+        p0 = p0 < n ? p0 : n;
+        p1 = p1 < n ? p1 : n;
+        const uint32_t none = (uint32_t)a.rows;  // sorts behind every row
+        const uint32_t before = p0 > 0 && p0 < n ? key_of(e[p0 - 1]) : none;
+        const uint32_t after = p1 < n ? key_of(e[p1]) : none;
+        uint32_t cur = p0 < p1 ? key_of(e[p0]) : none;
+        bool is_first = true, has_head = false, has_tail = false;
+        float acc[OCT];
+        zero_oct(acc);
+        const auto finish = [&](bool is_last) {
+            if (cur == none) return;
+            const bool h = is_first && before == cur, t = is_last && after == cur;
+            if (h) {
+                has_head = true;
+#pragma unroll
+                for (int c = 0; c < OCT; ++c) head[c][threadIdx.x] = acc[c];
+            } else if (t) {
+#pragma unroll
+                for (int c = 0; c < OCT; ++c) tail[c][threadIdx.x] = acc[c];
+            } else if (on) {
+                put_oct<TO>(a, cur, oct, acc);
+            }
+            has_tail = t;
+            if (is_last) through[team] = h && t;
+        };
+        through[team] = 0;
+        for (int64_t p = p0; p < p1; p += SUM_AHEAD) {
+            uint64_t x[SUM_AHEAD];
+            float v[SUM_AHEAD][OCT];
+#pragma unroll
+            for (int k = 0; k < SUM_AHEAD; ++k) x[k] = e[p + k < p1 ? p + k : p1 - 1];
+#pragma unroll
+            for (int k = 0; k < SUM_AHEAD; ++k)
+                grad_oct<TI>(a, (uint32_t)x[k], oct,
+                                   on && p + k < p1 && key_of(x[k]) != none, v[k]);
+#pragma unroll
+            for (int k = 0; k < SUM_AHEAD; ++k) {
+                if (p + k < p1) {
+                    if (key_of(x[k]) != cur) {
+                        finish(false);
+                        is_first = false;
+                        cur = key_of(x[k]);
+                        zero_oct(acc);
+                    }
+#pragma unroll
+                    for (int c = 0; c < OCT; ++c) acc[c] += v[k][c];
+                }
+            }
+        }
+        if (p0 < p1) finish(true);
+        __syncthreads();
+        // runs that begin before the block, then runs that begin in this team's piece
+        const int lane = (int)threadIdx.x % LPR;
+        const auto chain = [&](uint32_t key, int from, bool more, int slot) {
+            int j = from;
+            while (more && j < TEAMS) {
+#pragma unroll
+                for (int c = 0; c < OCT; ++c) acc[c] += head[c][j * LPR + lane];
+                more = through[j];
+                ++j;
+            }
+            if (slot == 1 && !more) {
+                if (on) put_oct<TO>(a, key, oct, acc);
+            } else if (on) {  // [0]: the rest of a run from before; [1]: the start of a longer one
+                float *p = part + (chunk * 2 + slot) * sh.part_ld + oct * OCT;
+                Pack<float, OCT> w;
+#pragma unroll
+                for (int c = 0; c < OCT; ++c) w.v[c] = acc[c];
+                __builtin_memcpy(p, &w, sizeof w);
+            }
+        };
+        if (team == 0 && has_head) {
+#pragma unroll
+            for (int c = 0; c < OCT; ++c) acc[c] = head[c][threadIdx.x];
+            chain(before, 1, through[0], 0);
+        }
+        if (has_tail && !through[team]) {
+#pragma unroll
+            for (int c = 0; c < OCT; ++c) acc[c] = tail[c][threadIdx.x];
+            chain(after, team + 1, true, 1);
+        }
+        return;
+    }
+    const int64_t b = (int64_t)blockIdx.x - sums;
+    const int64_t row0 = b / fill.stretches * fill.rows;
+    const int64_t row1 = row0 + fill.rows < a.rows ? row0 + fill.rows : a.rows;
+    // entries of the block's rows: 512 threads narrow both ends down
+    int64_t lo = 0, hi = n;
+    __shared__ int64_t ends[2];
+    if (threadIdx.x < 2)
+        ends[threadIdx.x] = first_at_least(e, 0, n, (uint32_t)(threadIdx.x ? row1 : row0));
+    __syncthreads();
+    lo = ends[0];
+    hi = ends[1];
+    for (int64_t r = row0 + threadIdx.x; r < row1; r += SUM_NT) {
+        const int64_t at = first_at_least(e, lo, hi, (uint32_t)r);
+        used[r - row0] = at < hi && key_of(e[at]) == (uint32_t)r;
+    }
+    __syncthreads();
+    float z[OCT];
+    zero_oct(z);
+    for (int u = threadIdx.x; u < FILL_UNITS; u += SUM_NT) {
+        int64_t row;
+        int32_t oct;
+        if (split_at(fill, b, u, row, oct) && !used[row - row0])
+            store_oct((TO *)a.out + row * a.out_ld + oct * OCT, oct_valid(a.dim, oct), z);
+    }
+}
+
+// A run that goes over the edge of chunk c and begins in it: its parts, in order.
+// Four waves take consecutive stretches of the parts.
+template <typename TO>
+__global__ void __launch_bounds__(BLOCK) k_grad_join(GradArgs a, const uint64_t *e, SumShape sh,
+                                                     int64_t step, const float *part)
+{
+    __shared__ float sum[3][SLAB];
+    const int32_t slabs = (int32_t)((a.dim + SLAB - 1) / SLAB);
+    const int64_t c = (int64_t)blockIdx.x / slabs;
+    const int32_t oct = (int32_t)(blockIdx.x % slabs) * WAVE + lane_id();
+    const int64_t edge = (c + 1) * step;
+    if (edge >= a.n) return;
+    const uint32_t key = key_of(e[edge]);
+    if (key == (uint32_t)a.rows || key_of(e[edge - 1]) != key) return;
+    if (c > 0 && key_of(e[c * step]) == key && key_of(e[c * step - 1]) == key) return;  // began earlier
+    int64_t parts = 0;  // chunks after c that the run reaches into
+    for (int64_t j = c + 1;; j += BLOCK) {
+        const int64_t at = (j + threadIdx.x) * step;
+        const int got = __syncthreads_count(at < a.n && key_of(e[at < a.n ? at : 0]) == key);
+        parts += got;
+        if (got < BLOCK) break;
+    }
+    const int64_t per = (parts + 3) / 4;
+    const int64_t j0 = c + 1 + wave_id() * per;
+    const int64_t j1 = j0 + per < c + 1 + parts ? j0 + per : c + 1 + parts;
+    const bool on = oct * OCT < a.dim;
+    float acc[OCT];
+    zero_oct(acc);
+    if (on) {
+        if (wave_id() == 0) load_oct(part + (c * 2 + 1) * sh.part_ld + oct * OCT, OCT, acc);
+        for (int64_t j = j0; j < j1; j += 4) {
+            float v[4][OCT];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                zero_oct(v[k]);
+                if (j + k < j1) load_oct(part + (j + k) * 2 * sh.part_ld + oct * OCT, OCT, v[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int q = 0; q < OCT; ++q) acc[q] += v[k][q];
+        }
+    }
+    if (wave_id() > 0) {
+#pragma unroll
+        for (int q = 0; q < OCT; ++q) sum[wave_id() - 1][q * WAVE + lane_id()] = acc[q];
+    }
+    __syncthreads();
+    if (wave_id() == 0 && on) {
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+#pragma unroll
+            for (int q = 0; q < OCT; ++q) acc[q] += sum[w][q * WAVE + lane_id()];
+        put_oct<TO>(a, key, oct, acc);
+    }
+}
+
+// ---------------------------------------------------------------- host
+
+static int team_lanes(int32_t dim)
+{
+    int l = 4;
+    while (l < WAVE && l * OCT < dim) l *= 2;
+    return l;
+}
+
+// Pieces of 4 to 32 entries per team: enough blocks for the card where there are few
+// entries, few cut runs where there are many.
+static SumShape sum_shape(int64_t n, int32_t dim)
+{
+    const int lpr = team_lanes(dim), teams = SUM_NT / lpr;
+    SumShape s;
+    s.slabs = (dim + lpr * OCT - 1) / (lpr * OCT);
+    int64_t per = n * s.slabs / ((int64_t)teams * 1024);
+    s.per = (int32_t)(per < 4 ? 4 : per > 32 ? 32 : per);
+    s.chunks = (n + (int64_t)s.per * teams - 1) / ((int64_t)s.per * teams);
+    s.part_ld = ((int64_t)dim + OCT - 1) / OCT * OCT;
+    return s;
+}
+
+struct GradWs {
+    int64_t e0, e1, hist, part, bytes;
+    int64_t tiles;
+};
+static GradWs grad_layout(int64_t n, int32_t dim)
+{
+    GradWs w{};
+    if (n <= DIRECT_MAX) return w;
+    const auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
+    w.tiles = (n + SORT_TILE - 1) / SORT_TILE;
+    w.e0 = 0;
+    w.e1 = up(n * 8);
+    w.hist = w.e1 + (n > RANK_MAX ? up(n * 8) : 0);
+    w.part = w.hist + (n > RANK_MAX ? up((w.tiles + 1) * BINS_MAX * 4) : 0);
+    const SumShape s = sum_shape(n, dim);
+    w.bytes = w.part + up(s.chunks * 2 * s.part_ld * 4);
+    return w;
+}
+
+int64_t grad_workspace(int64_t n, int64_t, int32_t dim) { return grad_layout(n, dim).bytes; }
+
+template <typename IX>
+static hipError_t sort_tokens(const GradArgs &a, const GradWs &w, uint64_t **sorted, hipStream_t s)
+{
+    uint64_t *e0 = (uint64_t *)(a.ws + w.e0), *e1 = (uint64_t *)(a.ws + w.e1);
+    if (a.n <= RANK_MAX) {
+        *sorted = e0;
+        return launch(k_grad_rank<IX>, dim3((unsigned)((a.n + WAVE - 1) / WAVE)), dim3(RANK_NT), s,
+                      (const IX *)a.tokens, (int32_t)a.n, a.rows, e0);
+    }
+    int bits = 1;
+    while (a.rows >> bits) ++bits;  // keys are 0 .. rows
+    const int passes = (bits + DIGIT_MAX - 1) / DIGIT_MAX, width = (bits + passes - 1) / passes;
+    uint32_t *hist = (uint32_t *)(a.ws + w.hist);
+    const dim3 grid((unsigned)w.tiles), block(SORT_NT);
+    const bool prefixed = w.tiles > SELF_TILES;
+    const void *in = a.tokens;
+    uint64_t *out = e0;
+    for (int p = 0; p < passes; ++p) {
+        const Digits d{p * width, width};
+        hipError_t r = p == 0 ? launch(k_grad_hist<IX, true>, grid, block, s, in, a.n, a.rows, d, hist)
+                              : launch(k_grad_hist<IX, false>, grid, block, s, in, a.n, a.rows, d, hist);
+        if (r == hipSuccess && prefixed)
+            r = launch(k_grad_prefix, dim3(1), block, s, hist, w.tiles, width);
+        if (r == hipSuccess)
+            r = p == 0 ? launch(k_grad_scatter<IX, true>, grid, block, s, in, a.n, a.rows, d,
+                                (const uint32_t *)hist, w.tiles, prefixed, out)
+                       : launch(k_grad_scatter<IX, false>, grid, block, s, in, a.n, a.rows, d,
+                                (const uint32_t *)hist, w.tiles, prefixed, out);
+        if (r != hipSuccess) return r;
+        *sorted = out;
+        in = out;
+        out = out == e0 ? e1 : e0;
+    }
+    return hipSuccess;
+}
+
+template <typename TI, typename TO, typename IX>
+static hipError_t run_grad_as(const GradArgs &a, hipStream_t s)
+{
+    const int64_t width = ((int64_t)a.dim + OCT - 1) / OCT;
+    const Split fill = split_rows(a.add ? 0 : a.rows, width, FILL_UNITS);
+    const int64_t fills = split_blocks(fill);
+    if (a.n <= DIRECT_MAX) {
+        const int32_t slabs = (int32_t)((a.dim + SLAB - 1) / SLAB);
+        const int64_t sums = a.n * slabs;
+        if (sums + fills == 0) return hipSuccess;
+        if (sums + fills > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+        return launch(k_grad_direct<TI, TO, IX>, dim3((unsigned)(sums + fills)), dim3(BLOCK), s,
+                      a, slabs, sums, fill);
+    }
+    const GradWs w = grad_layout(a.n, a.dim);
+    const SumShape sh = sum_shape(a.n, a.dim);
+    const int64_t sums = sh.chunks * sh.slabs;
+    if (sums + fills > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    uint64_t *e = nullptr;
+    hipError_t r = sort_tokens<IX>(a, w, &e, s);
+    if (r != hipSuccess) return r;
+    float *part = (float *)(a.ws + w.part);
+    const int lpr = team_lanes(a.dim);
+    const auto sum = [&](auto kern) {
+        return launch(kern, dim3((unsigned)(sums + fills)), dim3(SUM_NT), s, a, (const uint64_t *)e, sh,
+                      part, fill);
+    };
+    r = lpr == 4    ? sum(k_grad_sum<TI, TO, 4>)
+        : lpr == 8  ? sum(k_grad_sum<TI, TO, 8>)
+        : lpr == 16 ? sum(k_grad_sum<TI, TO, 16>)
+        : lpr == 32 ? sum(k_grad_sum<TI, TO, 32>)
+                    : sum(k_grad_sum<TI, TO, 64>);
+    if (r != hipSuccess || sh.chunks == 1) return r;
+    const int64_t slabs = (a.dim + SLAB - 1) / SLAB;
+    return launch(k_grad_join<TO>, dim3((unsigned)((sh.chunks - 1) * slabs)), dim3(BLOCK), s, a,
+                  (const uint64_t *)e, sh, (int64_t)sh.per * (SUM_NT / lpr), (const float *)part);
+}
+
+hipError_t run_grad(const GradArgs &a, hipStream_t s)
+{
+    return with_index(a.token_type, [&](auto ix) {
+        return with_type(a.grad_type, [&](auto ti) {
+            return with_type(a.out_type, [&](auto to) {
+                using IX = decltype(ix);
+                using TI = decltype(ti);
+                using TO = decltype(to);
+                return run_grad_as<TI, TO, IX>(a, s);
+            });
+        });
+    });
+}
+
+}  // namespace sp

@@ -1,0 +1,119 @@
+// Token tables: lookup with scaling and dropout, and dropout by itself.
+#include "sp_rows.h"
+
+namespace sp {
+
+// ---------------------------------------------------------------- lookup
+//
+// out[i] = factor * keep(i) * table[token[i]], rows of zeros where the token is
+// no row of the table (padding).  Bound by the bytes of the rows.
+template <typename TI, typename TO, typename IX, bool DROP>
+struct Lookup {
+    const IX *tokens;
+    const TI *table;
+    TO *out;
+    int64_t rows, table_ld, out_ld;
+    int32_t dim;
+    float factor;
+    Drop drop;
+    struct Regs {
+        float v[OCT];
+        bool live;
+    };
+    __device__ __forceinline__ void load(int64_t row, int32_t oct, Regs &g) const
+    {
+        const int64_t t = (int64_t)tokens[row];
+        g.live = t >= 0 && t < rows;
+        if (g.live) load_oct(table + t * table_ld + oct * OCT, oct_valid(dim, oct), g.v);
+    }
+    __device__ __forceinline__ void store(int64_t row, int32_t oct, Regs &g) const
+    {
+        uint32_t keep = g.live ? 0xFFu : 0u;
+        if (DROP) keep &= keep_oct(drop, (uint32_t)oct, (uint32_t)row);
+#pragma unroll
+        for (int k = 0; k < OCT; ++k) g.v[k] = keep >> k & 1u ? g.v[k] * factor : 0.f;
+        store_oct(out + row * out_ld + oct * OCT, oct_valid(dim, oct), g.v);
+    }
+};
+
+hipError_t run_lookup(const LookupArgs &a, hipStream_t s)
+{
+    return with_index(a.token_type, [&](auto ix) {
+        return with_type(a.table_type, [&](auto ti) {
+            return with_type(a.out_type, [&](auto to) {
+                using IX = decltype(ix);
+                using TI = decltype(ti);
+                using TO = decltype(to);
+                const auto go = [&](auto op) {
+                    op.tokens = (const IX *)a.tokens;
+                    op.table = (const TI *)a.table;
+                    op.out = (TO *)a.out;
+                    op.rows = a.rows;
+                    op.table_ld = a.table_ld;
+                    op.out_ld = a.out_ld;
+                    op.dim = a.dim;
+                    op.factor = a.factor;
+                    op.drop = a.drop;
+                    return run_octets(op, a.n, a.dim, s);
+                };
+                return a.drop.drop ? go(Lookup<TI, TO, IX, true>{})
+                                   : go(Lookup<TI, TO, IX, false>{});
+            });
+        });
+    });
+}
+
+// ---------------------------------------------------------------- dropout
+//
+// out = [residual +] factor * keep * x.  The backward pass is the same call on
+// the gradient: the mask is drawn again from seed, offset and place.
+template <typename T, bool RES>
+struct Dropout {
+    const T *x, *residual;
+    T *out;
+    int64_t x_ld, residual_ld, out_ld;
+    int32_t dim;
+    float factor;
+    Drop drop;
+    struct Regs {
+        float v[OCT], r[RES ? OCT : 1];
+    };
+    __device__ __forceinline__ void load(int64_t row, int32_t oct, Regs &g) const
+    {
+        load_oct(x + row * x_ld + (int64_t)oct * OCT, oct_valid(dim, oct), g.v);
+        if constexpr (RES)
+            load_oct(residual + row * residual_ld + (int64_t)oct * OCT, oct_valid(dim, oct), g.r);
+    }
+    __device__ __forceinline__ void store(int64_t row, int32_t oct, Regs &g) const
+    {
+        const uint32_t keep = keep_oct(drop, (uint32_t)oct, (uint32_t)row);
+#pragma unroll
+        for (int k = 0; k < OCT; ++k) {
+            g.v[k] = keep >> k & 1u ? g.v[k] * factor : 0.f;
+            if constexpr (RES) g.v[k] += g.r[k];
+        }
+        store_oct(out + row * out_ld + (int64_t)oct * OCT, oct_valid(dim, oct), g.v);
+    }
+};
+
+hipError_t run_dropout(const DropoutArgs &a, hipStream_t s)
+{
+    return with_type(a.type, [&](auto t) {
+        using T = decltype(t);
+        const auto go = [&](auto op) {
+            op.x = (const T *)a.x;
+            op.residual = (const T *)a.residual;
+            op.out = (T *)a.out;
+            op.x_ld = a.x_ld;
+            op.residual_ld = a.residual_ld;
+            op.out_ld = a.out_ld;
+            op.dim = a.dim;
+            op.factor = a.factor;
+            op.drop = a.drop;
+            return run_octets(op, a.n, a.dim, s);
+        };
+        return a.residual ? go(Dropout<T, true>{}) : go(Dropout<T, false>{});
+    });
+}
+
+}  // namespace sp

@@ -6,6 +6,8 @@
 
 namespace sp {
 
+int32_t set_error(int32_t code, const char *text);  // of a call without a context; returns code
+
 constexpr int MAX_TABLES = 64;
 constexpr int MAX_PF = 4;        // successor batches a plan may prefetch
 constexpr int MAX_WINDOW = 16;   // batches one plan may look at (lookahead <= 15)
