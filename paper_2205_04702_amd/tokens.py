@@ -62,9 +62,9 @@ def _type(table, t, what):
 def _rows(x, what, copy=True):
     """x as a matrix of its last dimension whose elements follow one another, and its row
     stride: x itself where its strides allow, else (inputs) a copy."""
-    if x.dim() == 0:
-        raise _bad(f"{what} has no dimension")
     if x.dim() != 2:
+        if x.dim() == 0:
+            raise _bad(f"{what} has no dimension")
         try:
             x = x.view(-1, x.shape[-1]) if x.numel() else x.reshape(0, x.shape[-1])
         except RuntimeError:
@@ -72,59 +72,61 @@ def _rows(x, what, copy=True):
                 raise _bad(f"{what}: its rows are not a constant stride apart") from None
             x = x.reshape(-1, x.shape[-1])
     n, d = x.shape
-    if (d > 1 and x.stride(1) != 1) or (n > 1 and x.stride(0) < d):
+    ld, step = x.stride()
+    if (d > 1 and step != 1) or (n > 1 and ld < d):
         if not copy:
             raise _bad(f"{what}: the elements of its rows do not follow one another")
-        x = x.contiguous()
-    return x, max(x.stride(0), d)  # (the stride of a single row may be anything)
+        x, ld = x.contiguous(), d
+    return x, (ld if ld > d else d)  # (the stride of a single row may be anything)
 
 
 def _flat(x):
-    return x if x.dim() == 1 and (x.stride(0) == 1 or x.shape[0] < 2) else x.reshape(-1).contiguous()
+    return x if x.dim() == 1 and x.is_contiguous() else x.reshape(-1).contiguous()
 
 
-class _On:
-    """The device and stream of a call: the tensors' device made current, temporaries and
-    outputs allocated for the stream that the call runs on."""
-    __slots__ = ("stream", "inside")
+def _stream(stream, first, others):
+    """The raw current stream of the tensors' device, where the call can go ahead on it; None
+    where another device or stream has to be made current first (_on)."""
+    index = first.get_device()
+    if index < 0:
+        raise _bad(f"tensors on {first.device}: the operators run on the GPU")
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise _bad(f"tensors on {first.device} and {t.device}")
+    if stream is None and torch._C._cuda_getDevice() == index:
+        return torch._C._cuda_getCurrentRawStream(index)
+    return None
 
-    def __init__(self, stream, first, *others):
-        dev = first.device
-        if dev.type != "cuda":
-            raise _bad(f"tensors on {dev}: the operators run on the GPU")
-        for t in others:
-            if t is not None and t.device != dev:
-                raise _bad(f"tensors on {dev} and {t.device}")
-        self.inside = None
-        if stream is not None:
-            if not isinstance(stream, torch.cuda.Stream):
-                stream = torch.cuda.ExternalStream(int(stream or 0), device=dev)
-            if stream.device != dev:
-                raise _bad(f"a stream of {stream.device}, tensors on {dev}")
-            self.inside = torch.cuda.stream(stream)
-        elif dev.index != torch.cuda.current_device():
-            self.inside = torch.cuda.device(dev)
 
-    def __enter__(self):
-        if self.inside is not None:
-            self.inside.__enter__()
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.inside is not None:
-            self.inside.__exit__(*exc)
+def _on(stream, first):
+    """Makes the tensors' device and the given stream current: outputs and temporaries then
+    belong to the stream that the call runs on."""
+    if stream is None:
+        return torch.cuda.device(first.device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=first.device) if int(stream) \
+            else torch.cuda.default_stream(first.device)
+    if stream.device != first.device:
+        raise _bad(f"a stream of {stream.device}, tensors on {first.device}")
+    return torch.cuda.stream(stream)
 
 
 def _output(out, shape, dtype, device):
     if out is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape) or (dtype is not None and out.dtype != dtype):
+    if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
         raise _bad(f"out is {tuple(out.shape)} {out.dtype}, {tuple(shape)} {dtype} is needed")
     return out
 
 
+def _workspace(size, device, *sizes):
+    need = C.c_int64()
+    _check(size(*sizes, C.byref(need)))
+    return torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+
+
 def _check(status):
-    if status != sp.SP_OK:
+    if status:
         sp._check(status)
 
 
@@ -133,20 +135,23 @@ def lookup(tokens, table, scale=1.0, p=0.0, seed=0, offset=0, dtype=None, out=No
 
     Tokens outside the table (padding, -1) give rows of zeros.  dtype: the output's
     (default: the table's)."""
-    L = _lib or _load()
+    st = _stream(stream, table, (tokens, out))
+    if st is None:
+        with _on(stream, table):
+            return lookup(tokens, table, scale, p, seed, offset, dtype, out)
     if table.dim() != 2:
         raise _bad(f"table has shape {tuple(table.shape)}: [rows, dim] is needed")
-    with _On(stream, table, tokens, out) as st:
-        ids = _flat(tokens)
-        w, ld = _rows(table, "table")
-        if dtype is None:
-            dtype = table.dtype if out is None else out.dtype
-        out = _output(out, (*tokens.shape, w.shape[1]), dtype, table.device)
-        o, old = _rows(out, "out", copy=False)
-        _check(L.sp_lookup(ids.data_ptr(), _type(_INDEX, tokens, "tokens"), ids.shape[0],
-                           w.data_ptr(), _type(_FLOAT, table, "table"), w.shape[0], w.shape[1], ld,
-                           scale, p, seed & _MASK, offset & _MASK, o.data_ptr(),
-                           _type(_FLOAT, dtype, "out"), old, st))
+    ids = _flat(tokens)
+    w, ld = _rows(table, "table")
+    rows, dim = w.shape
+    if dtype is None:
+        dtype = table.dtype if out is None else out.dtype
+    out = _output(out, (*tokens.shape, dim), dtype, table.device)
+    o, old = _rows(out, "out", copy=False)
+    _check((_lib or _load()).sp_lookup(
+        ids.data_ptr(), _type(_INDEX, tokens, "tokens"), ids.shape[0], w.data_ptr(),
+        _type(_FLOAT, table, "table"), rows, dim, ld, scale, p, seed & _MASK, offset & _MASK,
+        o.data_ptr(), _type(_FLOAT, dtype, "out"), old, st))
     return out
 
 
@@ -157,27 +162,28 @@ def lookup_grad(tokens, grad, rows, scale=1.0, p=0.0, seed=0, offset=0, dtype=No
 
     accumulate: the sums are added to `out`, rows without a token stay as they are.  dtype:
     the result's (default float32)."""
-    L = _lib or _load()
-    with _On(stream, grad, tokens, out) as st:
-        if tuple(grad.shape[:-1]) != tuple(tokens.shape):
-            raise _bad(f"tokens {tuple(tokens.shape)}, gradient {tuple(grad.shape)}")
-        if accumulate and out is None:
-            raise _bad("accumulate needs out")
-        ids = _flat(tokens)
-        g, ld = _rows(grad, "gradient")
-        n, dim = g.shape
-        if dtype is None:
-            dtype = torch.float32 if out is None else out.dtype
-        need = C.c_int64()
-        _check(L.sp_lookup_grad_workspace(n, rows, dim, C.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=grad.device) if need.value else None
-        out = _output(out, (rows, dim), dtype, grad.device)
-        o, old = _rows(out, "out", copy=False)
-        _check(L.sp_lookup_grad(ids.data_ptr(), _type(_INDEX, tokens, "tokens"), n, g.data_ptr(),
-                                _type(_FLOAT, grad, "gradient"), dim, ld, scale, p, seed & _MASK,
-                                offset & _MASK, o.data_ptr(), _type(_FLOAT, dtype, "out"), rows,
-                                old, int(accumulate), 0 if ws is None else ws.data_ptr(),
-                                need.value, st))
+    st = _stream(stream, grad, (tokens, out))
+    if st is None:
+        with _on(stream, grad):
+            return lookup_grad(tokens, grad, rows, scale, p, seed, offset, dtype, out, accumulate)
+    if grad.shape[:-1] != tokens.shape:
+        raise _bad(f"tokens {tuple(tokens.shape)}, gradient {tuple(grad.shape)}")
+    if accumulate and out is None:
+        raise _bad("accumulate needs out")
+    lib = _lib or _load()
+    ids = _flat(tokens)
+    g, ld = _rows(grad, "gradient")
+    n, dim = g.shape
+    if dtype is None:
+        dtype = torch.float32 if out is None else out.dtype
+    ws = _workspace(lib.sp_lookup_grad_workspace, grad.device, n, rows, dim)
+    out = _output(out, (rows, dim), dtype, grad.device)
+    o, old = _rows(out, "out", copy=False)
+    _check(lib.sp_lookup_grad(
+        ids.data_ptr(), _type(_INDEX, tokens, "tokens"), n, g.data_ptr(),
+        _type(_FLOAT, grad, "gradient"), dim, ld, scale, p, seed & _MASK, offset & _MASK,
+        o.data_ptr(), _type(_FLOAT, dtype, "out"), rows, old, 1 if accumulate else 0,
+        *((0, 0) if ws is None else (ws.data_ptr(), ws.shape[0])), st))
     return out
 
 
@@ -185,19 +191,23 @@ def dropout(x, p, seed, offset=0, residual=None, out=None, stream=None):
     """[residual +] dropout of x, whose mask is drawn from (seed, offset) and each element's
     place and never stored.  Its gradient to x is dropout(grad, p, seed, offset), the
     residual's is grad itself.  out may be x or residual."""
-    L = _lib or _load()
-    with _On(stream, x, residual, out) as st:
-        if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
+    st = _stream(stream, x, (residual, out))
+    if st is None:
+        with _on(stream, x):
+            return dropout(x, p, seed, offset, residual, out)
+    v, ld = _rows(x, "x")
+    r, rld = None, 0
+    if residual is not None:
+        if residual.shape != x.shape or residual.dtype != x.dtype:
             raise _bad(f"x {tuple(x.shape)} {x.dtype}, residual {tuple(residual.shape)} {residual.dtype}")
-        code = _type(_FLOAT, x, "x")
-        v, ld = _rows(x, "x")
-        r, rld = (None, 0) if residual is None else _rows(residual, "residual")
-        out = _output(out, x.shape, x.dtype, x.device)
-        o, old = _rows(out, "out", copy=False)
-        if v.shape[1]:
-            _check(L.sp_dropout(v.data_ptr(), code, v.shape[0], v.shape[1], ld,
-                                0 if r is None else r.data_ptr(), rld, p, seed & _MASK,
-                                offset & _MASK, o.data_ptr(), old, st))
+        r, rld = _rows(residual, "residual")
+    out = _output(out, x.shape, x.dtype, x.device)
+    o, old = _rows(out, "out", copy=False)
+    n, dim = v.shape
+    if dim:
+        _check((_lib or _load()).sp_dropout(
+            v.data_ptr(), _type(_FLOAT, x, "x"), n, dim, ld, 0 if r is None else r.data_ptr(), rld,
+            p, seed & _MASK, offset & _MASK, o.data_ptr(), old, st))
     return out
 
 
@@ -210,6 +220,7 @@ def empty_cache(slots, dim, group=None, dtype=torch.int8, device="cuda"):
 
 
 def _cache(q, scales):
+    """Bytes, their row stride, scales, theirs, columns per scale."""
     if q.dim() != 2 or scales.dim() != 2 or scales.shape[0] != q.shape[0] or not scales.shape[1] \
             or q.shape[1] % scales.shape[1]:
         raise _bad(f"cache {tuple(q.shape)}, scales {tuple(scales.shape)}: [slots, dim] and "
@@ -225,55 +236,66 @@ def cache_write(q, scales, x, slots, stream=None):
     """Quantises the rows of x [*slots.shape, dim] (dim may be several dimensions, as heads and
     their width) into the given slots (distinct; rows of a slot outside the cache, as -1, are
     left out)."""
-    L = _lib or _load()
-    with _On(stream, q, scales, x, slots) as st:
-        v, ld, s, sld, group = _cache(q, scales)
-        at = _flat(slots)
-        n, dim = at.shape[0], q.shape[1]
-        if x.shape[:slots.dim()] != slots.shape or x.numel() != n * dim:
-            raise _bad(f"cache {tuple(q.shape)}, {tuple(slots.shape)} slots, rows {tuple(x.shape)}")
+    st = _stream(stream, q, (scales, x, slots))
+    if st is None:
+        with _on(stream, q):
+            return cache_write(q, scales, x, slots)
+    v, ld, s, sld, group = _cache(q, scales)
+    at = _flat(slots)
+    n, (size, dim) = at.shape[0], v.shape
+    if x.shape[:slots.dim()] != slots.shape or x.numel() != n * dim:
+        raise _bad(f"cache {tuple(q.shape)}, {tuple(slots.shape)} slots, rows {tuple(x.shape)}")
+    r = x
+    if x.dim() != 2 or slots.dim() != 1:
         try:
             r = x.view(n, dim)
         except RuntimeError:
             r = x.reshape(n, dim)
-        r, rld = _rows(r, "x")
-        _check(L.sp_cache_write(r.data_ptr(), _type(_FLOAT, x, "x"), r.shape[0], r.shape[1], rld,
-                                at.data_ptr(), _type(_INDEX, slots, "slots"), group, v.data_ptr(),
-                                _type(_KIND, q, "cache"), v.shape[0], ld, s.data_ptr(), sld, st))
+    r, rld = _rows(r, "x")
+    _check((_lib or _load()).sp_cache_write(
+        r.data_ptr(), _type(_FLOAT, x, "x"), n, dim, rld, at.data_ptr(),
+        _type(_INDEX, slots, "slots"), group, v.data_ptr(), _type(_KIND, q, "cache"), size, ld,
+        s.data_ptr(), sld, st))
 
 
 def cache_read(q, scales, slots, dtype=torch.bfloat16, out=None, stream=None):
     """The rows [*slots.shape, dim] that the given slots stand for; zeros for a slot outside
     the cache (as -1)."""
-    L = _lib or _load()
-    with _On(stream, q, scales, slots, out) as st:
-        v, ld, s, sld, group = _cache(q, scales)
-        at = _flat(slots)
-        out = _output(out, (*slots.shape, q.shape[1]), dtype, q.device)
-        o, old = _rows(out, "out", copy=False)
-        _check(L.sp_cache_read(v.data_ptr(), _type(_KIND, q, "cache"), v.shape[0], v.shape[1], ld,
-                               s.data_ptr(), sld, group, at.data_ptr(),
-                               _type(_INDEX, slots, "slots"), at.shape[0], o.data_ptr(),
-                               _type(_FLOAT, dtype, "out"), old, st))
+    st = _stream(stream, q, (scales, slots, out))
+    if st is None:
+        with _on(stream, q):
+            return cache_read(q, scales, slots, dtype, out)
+    v, ld, s, sld, group = _cache(q, scales)
+    at = _flat(slots)
+    size, dim = v.shape
+    out = _output(out, (*slots.shape, dim), dtype, q.device)
+    o, old = _rows(out, "out", copy=False)
+    _check((_lib or _load()).sp_cache_read(
+        v.data_ptr(), _type(_KIND, q, "cache"), size, dim, ld, s.data_ptr(), sld, group,
+        at.data_ptr(), _type(_INDEX, slots, "slots"), at.shape[0], o.data_ptr(),
+        _type(_FLOAT, dtype, "out"), old, st))
     return out
 
 
 def quantize(x, group=None, dtype=torch.int8, stream=None):
     """The rows of x [..., dim] in 8 bits: bytes [n, dim] and scales [n, dim / group], laid out
     as empty_cache() does (group: the whole row)."""
-    L = _lib or _load()
-    with _On(stream, x) as st:
-        r, rld = _rows(x, "x")
-        n, dim = r.shape
-        group = group or dim
-        kind = _type(_KIND, dtype, "dtype")
-        if dim < 1 or group < 1 or dim % group:
-            raise _bad(f"group {group} does not divide dim {dim}")
-        ld = (dim + 15) // 16 * 16
-        q = torch.empty((n, ld), dtype=dtype, device=x.device)
-        scales = torch.empty((n, dim // group), dtype=torch.float32, device=x.device)
-        _check(L.sp_cache_write(r.data_ptr(), _type(_FLOAT, x, "x"), n, dim, rld, 0, 0, group,
-                                q.data_ptr(), kind, n, ld, scales.data_ptr(), dim // group, st))
+    st = _stream(stream, x, ())
+    if st is None:
+        with _on(stream, x):
+            return quantize(x, group, dtype)
+    r, rld = _rows(x, "x")
+    n, dim = r.shape
+    group = group or dim
+    kind = _type(_KIND, dtype, "dtype")
+    if dim < 1 or group < 1 or dim % group:
+        raise _bad(f"group {group} does not divide dim {dim}")
+    ld = (dim + 15) // 16 * 16
+    q = torch.empty((n, ld), dtype=dtype, device=x.device)
+    scales = torch.empty((n, dim // group), dtype=torch.float32, device=x.device)
+    _check((_lib or _load()).sp_cache_write(
+        r.data_ptr(), _type(_FLOAT, x, "x"), n, dim, rld, 0, 0, group, q.data_ptr(), kind, n, ld,
+        scales.data_ptr(), dim // group, st))
     return (q if ld == dim else q[:, :dim]), scales
 
 
@@ -281,26 +303,28 @@ def product(x, x_scales, w, w_scales, dtype=torch.bfloat16, out=None, stream=Non
     """x_scales[:, None] * w_scales * (x @ w.T) of 8-bit integer rows x [m, k] and w [n, k],
     the sums exact; one scale per row of each ([m] or [m, 1], [n] or [n, 1]).  Fastest where
     rows start at multiples of 16 bytes, as quantize() and empty_cache() lay them out."""
-    L = _lib or _load()
-    with _On(stream, x, x_scales, w, w_scales, out) as st:
-        if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
-            raise _bad(f"x {tuple(x.shape)}, w {tuple(w.shape)}: [m, k] and [n, k] are needed")
-        (m, k), n = x.shape, w.shape[0]
-        if x.dtype != torch.int8 or w.dtype != torch.int8:
-            raise _bad(f"x is {x.dtype}, w {w.dtype}: int8 is needed")
-        if x_scales.numel() != m or w_scales.numel() != n or x_scales.dtype != torch.float32 \
-                or w_scales.dtype != torch.float32:
-            raise _bad(f"scales {tuple(x_scales.shape)} {x_scales.dtype}, {tuple(w_scales.shape)} "
-                       f"{w_scales.dtype}: {m} and {n} of float32 are needed")
-        a, ald = _rows(x, "x")
-        b, bld = _rows(w, "w")
-        xs, ws = _flat(x_scales), _flat(w_scales)
-        need = C.c_int64()
-        _check(L.sp_product_workspace(m, n, k, C.byref(need)))
-        work = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
-        out = _output(out, (m, n), dtype, x.device)
-        o, old = _rows(out, "out", copy=False)
-        _check(L.sp_product(a.data_ptr(), xs.data_ptr(), m, ald, b.data_ptr(), ws.data_ptr(), n, bld,
-                            k, o.data_ptr(), _type(_FLOAT, dtype, "out"), old,
-                            0 if work is None else work.data_ptr(), need.value, st))
+    st = _stream(stream, x, (x_scales, w, w_scales, out))
+    if st is None:
+        with _on(stream, x):
+            return product(x, x_scales, w, w_scales, dtype, out)
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+        raise _bad(f"x {tuple(x.shape)}, w {tuple(w.shape)}: [m, k] and [n, k] are needed")
+    (m, k), n = x.shape, w.shape[0]
+    if x.dtype != torch.int8 or w.dtype != torch.int8:
+        raise _bad(f"x is {x.dtype}, w {w.dtype}: int8 is needed")
+    if x_scales.numel() != m or w_scales.numel() != n or x_scales.dtype != torch.float32 \
+            or w_scales.dtype != torch.float32:
+        raise _bad(f"scales {tuple(x_scales.shape)} {x_scales.dtype}, {tuple(w_scales.shape)} "
+                   f"{w_scales.dtype}: {m} and {n} of float32 are needed")
+    lib = _lib or _load()
+    a, ald = _rows(x, "x")
+    b, bld = _rows(w, "w")
+    xs, ws = _flat(x_scales), _flat(w_scales)
+    work = _workspace(lib.sp_product_workspace, x.device, m, n, k)
+    out = _output(out, (m, n), dtype, x.device)
+    o, old = _rows(out, "out", copy=False)
+    _check(lib.sp_product(
+        a.data_ptr(), xs.data_ptr(), m, ald, b.data_ptr(), ws.data_ptr(), n, bld, k, o.data_ptr(),
+        _type(_FLOAT, dtype, "out"), old, *((0, 0) if work is None else (work.data_ptr(), work.shape[0])),
+        st))
     return out
