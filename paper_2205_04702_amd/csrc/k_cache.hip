@@ -35,9 +35,8 @@ __device__ __forceinline__ uint2 pack_oct(const float (&v)[OCT])
 }
 
 template <int KIND>
-__device__ __forceinline__ void unpack_oct(uint2 w, float (&v)[OCT])
+__device__ __forceinline__ void unpack_oct(const uint32_t (&x)[2], float (&v)[OCT])
 {
-    const uint32_t x[2] = {w.x, w.y};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if constexpr (KIND == KIND_INT) {
@@ -62,19 +61,6 @@ __device__ __forceinline__ void store_bytes(uint8_t *p, int valid, uint2 w)
             if (k < valid) p[k] = (uint8_t)((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
     }
 }
-__device__ __forceinline__ uint2 load_bytes(const uint8_t *p, int valid)
-{
-    uint2 w = make_uint2(0, 0);
-    if (valid >= OCT) {
-        __builtin_memcpy(&w, p, 8);
-    } else {
-#pragma unroll
-        for (int k = 0; k < OCT; ++k)
-            if (k < valid) (k < 4 ? w.x : w.y) |= (uint32_t)p[k] << (8 * (k & 3));
-    }
-    return w;
-}
-
 // ---------------------------------------------------------------- write
 //
 // A team of TEAM lanes holds one group, OPL octets in each lane (team-strided,
@@ -105,7 +91,7 @@ __global__ void __launch_bounds__(BLOCK) k_cache_write(CacheArgs a, Split s, int
 #pragma unroll
         for (int i = 0; i < OPL; ++i) {
             const int32_t o = o0 + i * TEAM + lane;
-            if (o < octs) load_oct(x + o * OCT, oct_valid(a.group, o), v[i]);
+            if (o < octs) load_oct(x, o, cols_of(a.group), v[i]);
         }
 #pragma unroll
         for (int i = 0; i < OPL; ++i) {
@@ -113,7 +99,8 @@ __global__ void __launch_bounds__(BLOCK) k_cache_write(CacheArgs a, Split s, int
 #pragma unroll
                 for (int k = 0; k < OCT; ++k) {
                     const uint32_t b = __float_as_uint(v[i][k]) & 0x7FFFFFFFu;
-                    top_bits = b > top_bits ? b : top_bits;
+                    const bool in = (o0 + i * TEAM + lane) * OCT + k < a.group;
+                    top_bits = in && b > top_bits ? b : top_bits;
                 }
             }
         }
@@ -135,7 +122,7 @@ __global__ void __launch_bounds__(BLOCK) k_cache_write(CacheArgs a, Split s, int
             const int32_t o = o0 + i * TEAM + lane;
             if (o < octs) {
                 const int valid = oct_valid(a.group, o);
-                if (LOOP) load_oct(x + o * OCT, valid, v[i]);
+                if (LOOP) load_oct(x, o, cols_of(a.group), v[i]);
 #pragma unroll
                 for (int k = 0; k < OCT; ++k) v[i][k] = finite ? v[i][k] * inverse : 0.f;
                 store_bytes(q + o * OCT, valid, pack_oct<KIND>(v[i]));
@@ -187,28 +174,32 @@ struct CacheRead {
     CacheArgs a;
     float per_group;  // octets of a group, inverted; 0: one group
     struct Regs {
-        uint2 w;
+        Raw<uint8_t> w;
         float scale;
+        int64_t slot;
         bool live;
     };
-    __device__ __forceinline__ void load(int64_t row, int32_t oct, Regs &g) const
+    __device__ __forceinline__ void first(int64_t row, Regs &g) const
     {
-        const int64_t slot = a.index ? (int64_t)((const IX *)a.index)[row] : row;
-        g.live = slot >= 0 && slot < a.slots;
-        if (g.live) {
-            const int32_t grp = (int32_t)(((float)oct + 0.5f) * per_group);
-            g.scale = a.scales[slot * a.scales_ld + grp];
-            g.w = load_bytes((const uint8_t *)a.q + slot * a.q_ld + oct * OCT,
-                             oct_valid(a.dim, oct));
-        }
+        g.slot = a.index ? (int64_t)((const IX *)a.index)[row] : row;
     }
-    __device__ __forceinline__ void store(int64_t row, int32_t oct, Regs &g) const
+    __device__ __forceinline__ void load(int64_t, int32_t oct, Regs &g) const
+    {
+        g.live = g.slot >= 0 && g.slot < a.slots;
+        if (a.slots <= 0) return;  // the same for all
+        const int64_t slot = g.live ? g.slot : 0;
+        const int32_t grp = (int32_t)(((float)oct + 0.5f) * per_group);
+        g.scale = a.scales[slot * a.scales_ld + grp];
+        load_raw((const uint8_t *)a.q + slot * a.q_ld, oct, cols_of(a.dim), g.w);
+    }
+    __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
     {
         float v[OCT];
-        unpack_oct<KIND>(g.w, v);
+        settle(g.w, oct, cols_of(a.dim));
+        unpack_oct<KIND>(g.w.w, v);
 #pragma unroll
         for (int k = 0; k < OCT; ++k) v[k] = g.live ? v[k] * g.scale : 0.f;
-        store_oct((T *)a.x + row * a.x_ld + oct * OCT, oct_valid(a.dim, oct), v);
+        put_row_oct((T *)a.x + row * a.x_ld, oct, a.dim, fours, v);
     }
 };
 

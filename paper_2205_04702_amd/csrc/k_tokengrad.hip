@@ -35,38 +35,35 @@ __device__ __forceinline__ void zero_oct(float (&v)[OCT])
     for (int k = 0; k < OCT; ++k) v[k] = 0.f;
 }
 
-// The octet of one position, where the position is live, as dropout lets it through.
+// An octet of one position as loaded, added to the sums where it counts and dropout lets
+// it through.
 template <typename TI>
-__device__ __forceinline__ void grad_oct(const GradArgs &a, int64_t pos, int32_t oct, bool live,
-                                         float (&v)[OCT])
+__device__ __forceinline__ void add_oct(const GradArgs &a, Raw<TI> &r, int64_t pos, int32_t oct,
+                                        bool counts, float (&acc)[OCT])
 {
-    zero_oct(v);
-    if (!live) return;
-    load_oct((const TI *)a.grad + pos * a.grad_ld + oct * OCT, oct_valid(a.dim, oct), v);
-    if (a.drop.drop) {  // the same for the whole launch
-        const uint32_t keep = keep_oct(a.drop, (uint32_t)oct, (uint32_t)pos);
+    uint32_t keep = counts ? 0xFFu : 0u;
+    if (a.drop.drop) keep &= keep_oct(a.drop, (uint32_t)oct, (uint32_t)pos);  // the same for all
+    settle(r, oct, cols_of(a.dim));
 #pragma unroll
-        for (int k = 0; k < OCT; ++k) v[k] = keep >> k & 1u ? v[k] : 0.f;
-    }
+    for (int k = 0; k < OCT; ++k) acc[k] += keep >> k & 1u ? raw_float(r, k) : 0.f;
 }
 
-// A finished sum goes to its row of the table gradient.
+// A finished sum goes to its row of the table gradient (a team's lanes together).
 template <typename TO>
 __device__ __forceinline__ void put_oct(const GradArgs &a, int64_t row, int32_t oct,
                                         const float (&v)[OCT])
 {
-    TO *p = (TO *)a.out + row * a.out_ld + oct * OCT;
-    const int valid = oct_valid(a.dim, oct);
+    TO *p = (TO *)a.out + row * a.out_ld;
     float w[OCT];
     if (a.add) {
-        load_oct(p, valid, w);
+        load_oct(p, oct, cols_of(a.dim), w);
 #pragma unroll
         for (int k = 0; k < OCT; ++k) w[k] += a.factor * v[k];
     } else {
 #pragma unroll
         for (int k = 0; k < OCT; ++k) w[k] = a.factor * v[k];
     }
-    store_oct(p, valid, w);
+    put_row_oct(p, oct, a.dim, true, w);
 }
 
 // ---------------------------------------------------------------- few positions
@@ -75,7 +72,34 @@ __device__ __forceinline__ void put_oct(const GradArgs &a, int64_t row, int32_t 
 // position's token among all tokens, 64 at a time; the token's first position adds up
 // its rows (each wave those of every fourth group of 64 positions, joined in LDS).  The
 // other blocks write zeros to their rows without a token.
-constexpr int FILL_UNITS = 2048;  // octets that one block of a fill looks after
+constexpr int FILL_UNITS = 4096;  // 16-byte pieces of rows that one block of a fill looks after
+template <typename TO>
+constexpr int FILL_COLS = 16 / (int)sizeof(TO);
+
+// Zeros to the pieces of block b's rows that `used` does not name.  Pieces of 16 bytes,
+// so that a wave's store is one stretch: with octets, 32 bytes of fp32 per lane in two
+// stores, a fill of 1.07 GB ran at 4.3 TB/s.
+template <typename TO, int NT>
+__device__ __forceinline__ void fill_zeros(const GradArgs &a, const Split &fill, int64_t b,
+                                           int64_t row0, const uint8_t *used)
+{
+    constexpr int C = FILL_COLS<TO>;
+    Pack<TO, C> z;
+#pragma unroll
+    for (int k = 0; k < C; ++k) z.v[k] = from_float<TO>(0.f);
+#pragma unroll
+    for (int k = 0; k < FILL_UNITS / NT; ++k) {
+        int64_t row;
+        int32_t at;
+        if (!split_at(fill, b, k * NT + (int)threadIdx.x, row, at) || used[row - row0]) continue;
+        TO *p = (TO *)a.out + row * a.out_ld + at * C;
+        if (a.dim - at * C >= C) {
+            __builtin_memcpy(p, &z, sizeof z);
+        } else {
+            for (int k = 0; k < a.dim - at * C; ++k) p[k] = z.v[0];
+        }
+    }
+}
 template <typename TI, typename TO, typename IX>
 __global__ void __launch_bounds__(BLOCK) k_grad_direct(GradArgs a, int32_t slabs, int64_t sums,
                                                        Split fill)
@@ -107,17 +131,18 @@ __global__ void __launch_bounds__(BLOCK) k_grad_direct(GradArgs a, int32_t slabs
             if (g % 4 != wave_id()) continue;
             uint64_t m = mine[g];
             while (m) {
-                float v[4][OCT];
+                Raw<TI> v[4];
+                int p[4];
+                bool any[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int p = g * WAVE + __ffsll((unsigned long long)m) - 1;
-                    grad_oct<TI>(a, m ? p : 0, oct, on && m != 0, v[k]);
+                    any[k] = m != 0;
+                    p[k] = any[k] ? g * WAVE + __ffsll((unsigned long long)m) - 1 : i;
+                    load_raw((const TI *)a.grad + p[k] * a.grad_ld, on ? oct : 0, cols_of(a.dim), v[k]);
                     m &= m - 1;
                 }
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int c = 0; c < OCT; ++c) acc[c] += v[k][c];
+                for (int k = 0; k < 4; ++k) add_oct(a, v[k], p[k], oct, any[k], acc);
             }
         }
         if (wave_id() > 0) {
@@ -143,14 +168,7 @@ __global__ void __launch_bounds__(BLOCK) k_grad_direct(GradArgs a, int32_t slabs
         if (r >= 0 && r < fill.rows) used[r] = 1;
     }
     __syncthreads();
-    float z[OCT];
-    zero_oct(z);
-    for (int u = threadIdx.x; u < FILL_UNITS; u += BLOCK) {
-        int64_t row;
-        int32_t oct;
-        if (split_at(fill, b, u, row, oct) && !used[row - row0])
-            store_oct((TO *)a.out + row * a.out_ld + oct * OCT, oct_valid(a.dim, oct), z);
-    }
+    fill_zeros<TO, BLOCK>(a, fill, b, row0, used);
 }
 
 // ---------------------------------------------------------------- places by counting
@@ -345,9 +363,12 @@ __global__ void __launch_bounds__(SORT_NT) k_grad_scatter(const void *in, int64_
 // block, the first one) where the run begins adds them up in order; what crosses the
 // block's edges goes to `part`: [block][0] what continues from the block before,
 // [block][1] what begins here and continues.  Blocks after the sums write the zeros:
-// they find their rows' entries by bisection.
+// they search for their rows' entries.
 constexpr int SUM_NT = 512;
-constexpr int SUM_AHEAD = 8;
+constexpr int SUM_AHEAD = 8;  // entries whose rows a team has in flight
+
+// A value that is the same for a whole wave, held once for it.
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 struct SumShape {
     int32_t per;      // entries per team
@@ -355,6 +376,23 @@ struct SumShape {
     int64_t chunks;   // blocks along the entries
     int64_t part_ld;  // floats of one row of part
 };
+
+// First index whose key is at least `key`, else n: every lane of the wave looks at the
+// end of one of 64 pieces.
+__device__ __forceinline__ int64_t wave_first_at_least(const uint64_t *e, int64_t n, uint32_t key)
+{
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t step = (hi - lo + WAVE - 1) / WAVE, beg = lo + lane_id() * step;
+        const int64_t end = beg + step < hi ? beg + step : hi;
+        const bool less = beg < hi && key_of(e[beg < hi ? end - 1 : lo]) < key;
+        lo += (int64_t)__popcll(__ballot(less)) * step;  // (pieces below the key come first)
+        if (lo >= hi) return hi;
+        if (step == 1) return lo;
+        hi = lo + step < hi ? lo + step : hi;
+    }
+    return lo;
+}
 
 // First index in [lo, hi) whose key is at least `key`, else hi.
 __device__ __forceinline__ int64_t first_at_least(const uint64_t *e, int64_t lo, int64_t hi,
@@ -369,8 +407,9 @@ __device__ __forceinline__ int64_t first_at_least(const uint64_t *e, int64_t lo,
 }
 
 template <typename TI, typename TO, int LPR>
-__global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t *e, SumShape sh,
-                                                     float *part, Split fill)
+__global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t *__restrict__ e,
+                                                     SumShape sh, float *__restrict__ part,
+                                                     Split fill)
 {
     constexpr int TEAMS = SUM_NT / LPR;
     __shared__ float head[OCT][SUM_NT], tail[OCT][SUM_NT];
@@ -379,7 +418,8 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
     const int64_t n = a.n, sums = sh.chunks * sh.slabs;
     if ((int64_t)blockIdx.x < sums) {
         const int64_t chunk = (int64_t)blockIdx.x / sh.slabs;
-        const int team = (int)threadIdx.x / LPR;
+        // with a whole wave per team its entries, places and branches are the wave's
+        const int team = LPR == WAVE ? scalar(wave_id()) : (int)threadIdx.x / LPR;
         const int32_t oct = (int32_t)(blockIdx.x % sh.slabs) * LPR + (int)threadIdx.x % LPR;
         const bool on = oct * OCT < a.dim;
         const int64_t c0 = chunk * sh.per * TEAMS;
@@ -412,13 +452,13 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
         through[team] = 0;
         for (int64_t p = p0; p < p1; p += SUM_AHEAD) {
             uint64_t x[SUM_AHEAD];
-            float v[SUM_AHEAD][OCT];
+            Raw<TI> v[SUM_AHEAD];
 #pragma unroll
             for (int k = 0; k < SUM_AHEAD; ++k) x[k] = e[p + k < p1 ? p + k : p1 - 1];
 #pragma unroll
             for (int k = 0; k < SUM_AHEAD; ++k)
-                grad_oct<TI>(a, (uint32_t)x[k], oct,
-                                   on && p + k < p1 && key_of(x[k]) != none, v[k]);
+                load_raw((const TI *)a.grad + (int64_t)(uint32_t)x[k] * a.grad_ld, on ? oct : 0,
+                         cols_of(a.dim), v[k]);
 #pragma unroll
             for (int k = 0; k < SUM_AHEAD; ++k) {
                 if (p + k < p1) {
@@ -428,8 +468,7 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
                         cur = key_of(x[k]);
                         zero_oct(acc);
                     }
-#pragma unroll
-                    for (int c = 0; c < OCT; ++c) acc[c] += v[k][c];
+                    add_oct(a, v[k], (uint32_t)x[k], oct, true, acc);
                 }
             }
         }
@@ -470,27 +509,25 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
     const int64_t b = (int64_t)blockIdx.x - sums;
     const int64_t row0 = b / fill.stretches * fill.rows;
     const int64_t row1 = row0 + fill.rows < a.rows ? row0 + fill.rows : a.rows;
-    // entries of the block's rows: 512 threads narrow both ends down
-    int64_t lo = 0, hi = n;
+    // the entries of the block's rows, between two searches, say which rows have one
     __shared__ int64_t ends[2];
-    if (threadIdx.x < 2)
-        ends[threadIdx.x] = first_at_least(e, 0, n, (uint32_t)(threadIdx.x ? row1 : row0));
+    if (wave_id() < 2) {
+        const int64_t at = wave_first_at_least(e, n, (uint32_t)(wave_id() ? row1 : row0));
+        if (lane_id() == 0) ends[wave_id()] = at;
+    }
+    for (int u = threadIdx.x; u < FILL_UNITS; u += SUM_NT) used[u] = 0;
     __syncthreads();
-    lo = ends[0];
-    hi = ends[1];
-    for (int64_t r = row0 + threadIdx.x; r < row1; r += SUM_NT) {
-        const int64_t at = first_at_least(e, lo, hi, (uint32_t)r);
-        used[r - row0] = at < hi && key_of(e[at]) == (uint32_t)r;
+    const int64_t lo = ends[0], hi = ends[1];
+    if (hi - lo <= 4 * SUM_NT) {
+        for (int64_t i = lo + threadIdx.x; i < hi; i += SUM_NT) used[key_of(e[i]) - row0] = 1;
+    } else {
+        for (int64_t r = row0 + threadIdx.x; r < row1; r += SUM_NT) {
+            const int64_t at = first_at_least(e, lo, hi, (uint32_t)r);
+            used[r - row0] = at < hi && key_of(e[at]) == (uint32_t)r;
+        }
     }
     __syncthreads();
-    float z[OCT];
-    zero_oct(z);
-    for (int u = threadIdx.x; u < FILL_UNITS; u += SUM_NT) {
-        int64_t row;
-        int32_t oct;
-        if (split_at(fill, b, u, row, oct) && !used[row - row0])
-            store_oct((TO *)a.out + row * a.out_ld + oct * OCT, oct_valid(a.dim, oct), z);
-    }
+    fill_zeros<TO, SUM_NT>(a, fill, b, row0, used);
 }
 
 // A run that goes over the edge of chunk c and begins in it: its parts, in order.
@@ -519,21 +556,20 @@ __global__ void __launch_bounds__(BLOCK) k_grad_join(GradArgs a, const uint64_t 
     const int64_t j0 = c + 1 + wave_id() * per;
     const int64_t j1 = j0 + per < c + 1 + parts ? j0 + per : c + 1 + parts;
     const bool on = oct * OCT < a.dim;
+    const Cols whole = cols_of((int32_t)sh.part_ld);  // rows of part are whole octets
     float acc[OCT];
     zero_oct(acc);
     if (on) {
-        if (wave_id() == 0) load_oct(part + (c * 2 + 1) * sh.part_ld + oct * OCT, OCT, acc);
+        if (wave_id() == 0) load_oct(part + (c * 2 + 1) * sh.part_ld, oct, whole, acc);
         for (int64_t j = j0; j < j1; j += 4) {
-            float v[4][OCT];
+            Raw<float> v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                zero_oct(v[k]);
-                if (j + k < j1) load_oct(part + (j + k) * 2 * sh.part_ld + oct * OCT, OCT, v[k]);
-            }
+            for (int k = 0; k < 4; ++k)
+                load_raw(part + (j + k < j1 ? j + k : j) * 2 * sh.part_ld, oct, whole, v[k]);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int q = 0; q < OCT; ++q) acc[q] += v[k][q];
+                for (int q = 0; q < OCT; ++q) acc[q] += j + k < j1 ? raw_float(v[k], q) : 0.f;
         }
     }
     if (wave_id() > 0) {
@@ -633,7 +669,7 @@ static hipError_t sort_tokens(const GradArgs &a, const GradWs &w, uint64_t **sor
 template <typename TI, typename TO, typename IX>
 static hipError_t run_grad_as(const GradArgs &a, hipStream_t s)
 {
-    const int64_t width = ((int64_t)a.dim + OCT - 1) / OCT;
+    const int64_t width = ((int64_t)a.dim + FILL_COLS<TO> - 1) / FILL_COLS<TO>;
     const Split fill = split_rows(a.add ? 0 : a.rows, width, FILL_UNITS);
     const int64_t fills = split_blocks(fill);
     if (a.n <= DIRECT_MAX) {

@@ -17,22 +17,26 @@ struct Lookup {
     float factor;
     Drop drop;
     struct Regs {
-        float v[OCT];
+        Raw<TI> r;
+        int64_t t;
         bool live;
     };
-    __device__ __forceinline__ void load(int64_t row, int32_t oct, Regs &g) const
+    __device__ __forceinline__ void first(int64_t row, Regs &g) const { g.t = (int64_t)tokens[row]; }
+    __device__ __forceinline__ void load(int64_t, int32_t oct, Regs &g) const
     {
-        const int64_t t = (int64_t)tokens[row];
-        g.live = t >= 0 && t < rows;
-        if (g.live) load_oct(table + t * table_ld + oct * OCT, oct_valid(dim, oct), g.v);
+        g.live = g.t >= 0 && g.t < rows;
+        if (rows > 0) load_raw(table + (g.live ? g.t : 0) * table_ld, oct, cols_of(dim), g.r);
     }
-    __device__ __forceinline__ void store(int64_t row, int32_t oct, Regs &g) const
+    __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
     {
         uint32_t keep = g.live ? 0xFFu : 0u;
         if (DROP) keep &= keep_oct(drop, (uint32_t)oct, (uint32_t)row);
+        float v[OCT];
+        settle(g.r, oct, cols_of(dim));
+        raw_floats(g.r, v);
 #pragma unroll
-        for (int k = 0; k < OCT; ++k) g.v[k] = keep >> k & 1u ? g.v[k] * factor : 0.f;
-        store_oct(out + row * out_ld + oct * OCT, oct_valid(dim, oct), g.v);
+        for (int k = 0; k < OCT; ++k) v[k] = keep >> k & 1u ? v[k] * factor : 0.f;
+        put_row_oct(out + row * out_ld, oct, dim, fours, v);
     }
 };
 
@@ -76,23 +80,30 @@ struct Dropout {
     float factor;
     Drop drop;
     struct Regs {
-        float v[OCT], r[RES ? OCT : 1];
+        Raw<T> x, r;
     };
+    __device__ __forceinline__ void first(int64_t, Regs &) const {}
     __device__ __forceinline__ void load(int64_t row, int32_t oct, Regs &g) const
     {
-        load_oct(x + row * x_ld + (int64_t)oct * OCT, oct_valid(dim, oct), g.v);
-        if constexpr (RES)
-            load_oct(residual + row * residual_ld + (int64_t)oct * OCT, oct_valid(dim, oct), g.r);
+        load_raw(x + row * x_ld, oct, cols_of(dim), g.x);
+        if (RES) load_raw(residual + row * residual_ld, oct, cols_of(dim), g.r);
     }
-    __device__ __forceinline__ void store(int64_t row, int32_t oct, Regs &g) const
+    __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
     {
         const uint32_t keep = keep_oct(drop, (uint32_t)oct, (uint32_t)row);
+        float v[OCT], r[OCT];
+        settle(g.x, oct, cols_of(dim));
+        raw_floats(g.x, v);
+        if (RES) {
+            settle(g.r, oct, cols_of(dim));
+            raw_floats(g.r, r);
+        }
 #pragma unroll
         for (int k = 0; k < OCT; ++k) {
-            g.v[k] = keep >> k & 1u ? g.v[k] * factor : 0.f;
-            if constexpr (RES) g.v[k] += g.r[k];
+            v[k] = keep >> k & 1u ? v[k] * factor : 0.f;
+            if (RES) v[k] += r[k];
         }
-        store_oct(out + row * out_ld + (int64_t)oct * OCT, oct_valid(dim, oct), g.v);
+        put_row_oct(out + row * out_ld, oct, dim, fours, v);
     }
 };
 

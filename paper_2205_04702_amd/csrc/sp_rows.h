@@ -44,18 +44,96 @@ __device__ __forceinline__ float to_float(T x) { return (float)x; }
 template <typename T>
 __device__ __forceinline__ T from_float(float x) { return (T)x; }  // to nearest, ties to even
 
+// An octet as it lies in memory.  Loads come without a branch around them, so that those
+// of a thread are in flight together, and are turned into numbers when they are
+// used: with the conversion beside the load, every load was waited for by itself.
 template <typename T>
-__device__ __forceinline__ void load_oct(const T *p, int valid, float (&v)[OCT])
+struct Raw {
+    static constexpr int WORDS = (int)sizeof(T) * OCT / 4;
+    uint32_t w[WORDS];
+};
+
+// The columns of a row, as octets.  The last octet of a row of 8 columns or more is loaded
+// as the row's last eight columns and moved down (settle); a narrower row, value by value.
+struct Cols {
+    int32_t dim;
+    int32_t over;  // columns that the last octet lacks, 0 .. 7
+};
+__device__ __forceinline__ Cols cols_of(int32_t dim) { return Cols{dim, -dim & (OCT - 1)}; }
+__device__ __forceinline__ int oct_valid(int32_t dim, int32_t oct)
 {
-    if (valid >= OCT) {
-        Pack<T, OCT> w;
-        __builtin_memcpy(&w, p, sizeof w);
+    const int v = dim - oct * OCT;
+    return v < OCT ? v : OCT;
+}
+
+template <typename T>
+__device__ __forceinline__ void load_raw(const T *row, int32_t oct, const Cols &c, Raw<T> &r)
+{
+    if (c.dim >= OCT) {
+        const int32_t col = oct * OCT, last = c.dim - OCT;
+        __builtin_memcpy(r.w, row + (col < last ? col : last), sizeof r.w);
+    } else {  // last value first, each moving the later ones up (few registers, no speed)
+        constexpr int N = Raw<T>::WORDS, UP = (4 - (int)sizeof(T)) & 3;
 #pragma unroll
-        for (int k = 0; k < OCT; ++k) v[k] = to_float(w.v[k]);
-    } else {
+        for (int i = 0; i < N; ++i) r.w[i] = 0;
+#pragma unroll 1
+        for (int k = c.dim - 1; k >= 0; --k) {
+            T x = row[k];
+            uint32_t bits = 0;
+            __builtin_memcpy(&bits, &x, sizeof x);
 #pragma unroll
-        for (int k = 0; k < OCT; ++k) v[k] = k < valid ? to_float(p[k]) : 0.f;
+            for (int i = N - 1; i > 0; --i)
+                r.w[i] = UP ? __builtin_amdgcn_alignbyte(r.w[i], r.w[i - 1], UP) : r.w[i - 1];
+            r.w[0] = UP ? r.w[0] << (8 * (4 - UP)) | bits : bits;
+        }
     }
+}
+
+// What was loaded for octet `oct`, its first columns first (beyond the row: anything).
+template <typename T>
+__device__ __forceinline__ void settle(Raw<T> &r, int32_t oct, const Cols &c)
+{
+    if (c.over == 0 || c.dim < OCT) return;  // the same for all
+    const bool tail = oct * OCT > c.dim - OCT;
+    const int bytes = c.over * (int)sizeof(T);
+    constexpr int N = Raw<T>::WORDS;
+#pragma unroll
+    for (int by = 4; by < N * 4; by *= 2) {
+        const bool move = tail && (bytes & by);
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.w[i] = move ? (i + by / 4 < N ? r.w[i + by / 4] : 0u) : r.w[i];
+    }
+    if (sizeof(T) < 4) {
+        const int sh = tail ? (bytes & 3) : 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            r.w[i] = __builtin_amdgcn_alignbyte(i + 1 < N ? r.w[i + 1] : 0u, r.w[i], sh);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ float raw_float(const Raw<T> &r, int k)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(r.w[k]);
+    const uint16_t h = (uint16_t)(r.w[k / 2] >> (k % 2 * 16));
+    T t;
+    __builtin_memcpy(&t, &h, sizeof(T) < 4 ? sizeof t : 0);
+    return to_float(t);
+}
+template <typename T>
+__device__ __forceinline__ void raw_floats(const Raw<T> &r, float (&v)[OCT])
+{
+#pragma unroll
+    for (int k = 0; k < OCT; ++k) v[k] = raw_float(r, k);
+}
+
+template <typename T>
+__device__ __forceinline__ void load_oct(const T *row, int32_t oct, const Cols &c, float (&v)[OCT])
+{
+    Raw<T> r;
+    load_raw(row, oct, c, r);
+    settle(r, oct, c);
+    raw_floats(r, v);
 }
 
 template <typename T>
@@ -71,6 +149,42 @@ __device__ __forceinline__ void store_oct(T *p, int valid, const float (&v)[OCT]
         for (int k = 0; k < OCT; ++k)
             if (k < valid) p[k] = from_float<T>(v[k]);
     }
+}
+
+// The value that lane CTRL's two bits for this lane name, among each four lanes.
+template <int CTRL>
+__device__ __forceinline__ float of_four(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+
+// Stores octet `oct` of a row of dim columns.  fours: each four lanes (4i .. 4i + 3) that get
+// here hold the octets 4j .. 4j + 3 of one row as far as it has them.  An octet of fp32
+// is two 16-byte stores; the four lanes first exchange halves, so that each of the
+// stores covers 64 consecutive bytes of four lanes and not every other 16.
+template <typename T>
+__device__ __forceinline__ void put_row_oct(T *row, int32_t oct, int32_t dim, bool fours,
+                                            const float (&v)[OCT])
+{
+    if constexpr (sizeof(T) == 4) {
+        if (fours && (oct | 3) * OCT + OCT <= dim) {
+            const bool odd = threadIdx.x & 1;
+            Pack<T, 4> a, b;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float a0 = of_four<0x50>(v[k]), a1 = of_four<0x50>(v[4 + k]);  // lanes 0 0 1 1
+                const float b0 = of_four<0xFA>(v[k]), b1 = of_four<0xFA>(v[4 + k]);  // lanes 2 2 3 3
+                a.v[k] = odd ? a1 : a0;
+                b.v[k] = odd ? b1 : b0;
+            }
+            T *p = row + (int64_t)(oct & ~3) * OCT + (threadIdx.x & 3) * 4;
+            __builtin_memcpy(p, &a, sizeof a);
+            __builtin_memcpy(p + 16, &b, sizeof b);
+            return;
+        }
+    }
+    const int left = dim - oct * OCT;
+    store_oct(row + (int64_t)oct * OCT, left < OCT ? left : OCT, v);
 }
 
 // ---------------------------------------------------------------- dropout
@@ -156,7 +270,8 @@ __device__ __forceinline__ bool split_at(const Split &s, int64_t b, int u, int64
     return r < s.rows && row < s.n && at < s.width;
 }
 
-// Every octet of a split through op: the loads of a thread's U octets first.
+// Every octet of a split through op: the loads of a thread's U octets first (those of
+// units that are none take the place of the block's first).
 template <class Op, int U>
 __global__ void __launch_bounds__(BLOCK) k_octets(Op op, Split s)
 {
@@ -167,11 +282,14 @@ __global__ void __launch_bounds__(BLOCK) k_octets(Op op, Split s)
 #pragma unroll
     for (int k = 0; k < U; ++k) {
         on[k] = split_at(s, blockIdx.x, k * BLOCK + (int)threadIdx.x, row[k], at[k]);
-        if (on[k]) op.load(row[k], at[k], g[k]);
+        if (!on[k]) split_at(s, blockIdx.x, 0, row[k], at[k]);
+        op.first(row[k], g[k]);
     }
 #pragma unroll
+    for (int k = 0; k < U; ++k) op.load(row[k], at[k], g[k]);
+#pragma unroll
     for (int k = 0; k < U; ++k)
-        if (on[k]) op.store(row[k], at[k], g[k]);
+        if (on[k]) op.store(row[k], at[k], s.span % 4 == 0, g[k]);
 }
 
 // With fewer octets than fill the card four times over, one octet per thread.
@@ -187,12 +305,6 @@ inline hipError_t run_octets(const Op &op, int64_t n, int64_t dim, hipStream_t s
     if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
     return deep ? launch(k_octets<Op, 4>, dim3((unsigned)blocks), dim3(BLOCK), st, op, s)
                 : launch(k_octets<Op, 1>, dim3((unsigned)blocks), dim3(BLOCK), st, op, s);
-}
-
-__device__ __forceinline__ int oct_valid(int32_t dim, int32_t oct)
-{
-    const int v = dim - oct * OCT;
-    return v < OCT ? v : OCT;
 }
 
 // ---------------------------------------------------------------- element types
