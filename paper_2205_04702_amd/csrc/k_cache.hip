@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(BLOCK) k_cache_write(CacheArgs a, Split s, int
 #pragma unroll
         for (int i = 0; i < OPL; ++i) {
             const int32_t o = o0 + i * TEAM + lane;
-            if (o < octs) load_oct(x, o, cols_of(a.group), v[i]);
+            if (o < octs) load_oct<true>(x, o, cols_of(a.group), v[i]);
         }
 #pragma unroll
         for (int i = 0; i < OPL; ++i) {
@@ -183,6 +183,7 @@ struct CacheRead {
     {
         g.slot = a.index ? (int64_t)((const IX *)a.index)[row] : row;
     }
+    template <bool STREAM>
     __device__ __forceinline__ void load(int64_t, int32_t oct, Regs &g) const
     {
         g.live = g.slot >= 0 && g.slot < a.slots;
@@ -192,6 +193,7 @@ struct CacheRead {
         g.scale = a.scales[slot * a.scales_ld + grp];
         load_raw((const uint8_t *)a.q + slot * a.q_ld, oct, cols_of(a.dim), g.w);
     }
+    template <bool STREAM>
     __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
     {
         float v[OCT];
@@ -199,7 +201,7 @@ struct CacheRead {
         unpack_oct<KIND>(g.w.w, v);
 #pragma unroll
         for (int k = 0; k < OCT; ++k) v[k] = g.live ? v[k] * g.scale : 0.f;
-        put_row_oct((T *)a.x + row * a.x_ld, oct, a.dim, fours, v);
+        put_row_oct<STREAM>((T *)a.x + row * a.x_ld, oct, a.dim, fours, v);
     }
 };
 

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(BLOCK) k_grad_direct(GradArgs a, int32_t slabs
                 for (int k = 0; k < 4; ++k) {
                     any[k] = m != 0;
                     p[k] = any[k] ? g * WAVE + __ffsll((unsigned long long)m) - 1 : i;
-                    load_raw((const TI *)a.grad + p[k] * a.grad_ld, on ? oct : 0, cols_of(a.dim), v[k]);
+                    load_raw<true>((const TI *)a.grad + p[k] * a.grad_ld, on ? oct : 0, cols_of(a.dim), v[k]);
                     m &= m - 1;
                 }
 #pragma unroll
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
             for (int k = 0; k < SUM_AHEAD; ++k) x[k] = e[p + k < p1 ? p + k : p1 - 1];
 #pragma unroll
             for (int k = 0; k < SUM_AHEAD; ++k)
-                load_raw((const TI *)a.grad + (int64_t)(uint32_t)x[k] * a.grad_ld, on ? oct : 0,
+                load_raw<true>((const TI *)a.grad + (int64_t)(uint32_t)x[k] * a.grad_ld, on ? oct : 0,
                          cols_of(a.dim), v[k]);
 #pragma unroll
             for (int k = 0; k < SUM_AHEAD; ++k) {

@@ -22,11 +22,13 @@ struct Lookup {
         bool live;
     };
     __device__ __forceinline__ void first(int64_t row, Regs &g) const { g.t = (int64_t)tokens[row]; }
+    template <bool STREAM>
     __device__ __forceinline__ void load(int64_t, int32_t oct, Regs &g) const
     {
         g.live = g.t >= 0 && g.t < rows;
         if (rows > 0) load_raw(table + (g.live ? g.t : 0) * table_ld, oct, cols_of(dim), g.r);
     }
+    template <bool STREAM>
     __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
     {
         uint32_t keep = g.live ? 0xFFu : 0u;
@@ -36,7 +38,7 @@ struct Lookup {
         raw_floats(g.r, v);
 #pragma unroll
         for (int k = 0; k < OCT; ++k) v[k] = keep >> k & 1u ? v[k] * factor : 0.f;
-        put_row_oct(out + row * out_ld, oct, dim, fours, v);
+        put_row_oct<STREAM>(out + row * out_ld, oct, dim, fours, v);
     }
 };
 
@@ -83,11 +85,13 @@ struct Dropout {
         Raw<T> x, r;
     };
     __device__ __forceinline__ void first(int64_t, Regs &) const {}
+    template <bool STREAM>
     __device__ __forceinline__ void load(int64_t row, int32_t oct, Regs &g) const
     {
-        load_raw(x + row * x_ld, oct, cols_of(dim), g.x);
-        if (RES) load_raw(residual + row * residual_ld, oct, cols_of(dim), g.r);
+        load_raw<STREAM>(x + row * x_ld, oct, cols_of(dim), g.x);
+        if (RES) load_raw<STREAM>(residual + row * residual_ld, oct, cols_of(dim), g.r);
     }
+    template <bool STREAM>
     __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
     {
         const uint32_t keep = keep_oct(drop, (uint32_t)oct, (uint32_t)row);
@@ -103,7 +107,7 @@ struct Dropout {
             v[k] = keep >> k & 1u ? v[k] * factor : 0.f;
             if (RES) v[k] += r[k];
         }
-        put_row_oct(out + row * out_ld, oct, dim, fours, v);
+        put_row_oct<STREAM>(out + row * out_ld, oct, dim, fours, v);
     }
 };
 

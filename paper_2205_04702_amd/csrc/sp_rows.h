@@ -39,6 +39,38 @@ struct Pack {
     T v[N];
 };
 
+// Moves of 16 bytes at any address.  STREAM: past the caches, for what is read or written
+// once and is more than they hold; kept in them it would only displace what is read again.
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+typedef uint32_t word4_any __attribute__((ext_vector_type(4), aligned(1)));
+template <bool STREAM, int BYTES>
+__device__ __forceinline__ void get_bytes(void *to, const void *from)
+{
+    if constexpr (STREAM && BYTES % 16 == 0) {
+#pragma unroll
+        for (int i = 0; i < BYTES / 16; ++i) {
+            const word4 x = __builtin_nontemporal_load((const word4_any *)from + i);
+            __builtin_memcpy((char *)to + 16 * i, &x, 16);
+        }
+    } else {
+        __builtin_memcpy(to, from, BYTES);
+    }
+}
+template <bool STREAM, int BYTES>
+__device__ __forceinline__ void put_bytes(void *to, const void *from)
+{
+    if constexpr (STREAM && BYTES % 16 == 0) {
+#pragma unroll
+        for (int i = 0; i < BYTES / 16; ++i) {
+            word4 x;
+            __builtin_memcpy(&x, (const char *)from + 16 * i, 16);
+            __builtin_nontemporal_store((word4_any)x, (word4_any *)to + i);
+        }
+    } else {
+        __builtin_memcpy(to, from, BYTES);
+    }
+}
+
 template <typename T>
 __device__ __forceinline__ float to_float(T x) { return (float)x; }
 template <typename T>
@@ -66,12 +98,12 @@ __device__ __forceinline__ int oct_valid(int32_t dim, int32_t oct)
     return v < OCT ? v : OCT;
 }
 
-template <typename T>
+template <bool STREAM = false, typename T>
 __device__ __forceinline__ void load_raw(const T *row, int32_t oct, const Cols &c, Raw<T> &r)
 {
     if (c.dim >= OCT) {
         const int32_t col = oct * OCT, last = c.dim - OCT;
-        __builtin_memcpy(r.w, row + (col < last ? col : last), sizeof r.w);
+        get_bytes<STREAM, sizeof r.w>(r.w, row + (col < last ? col : last));
     } else {  // last value first, each moving the later ones up (few registers, no speed)
         constexpr int N = Raw<T>::WORDS, UP = (4 - (int)sizeof(T)) & 3;
 #pragma unroll
@@ -127,23 +159,23 @@ __device__ __forceinline__ void raw_floats(const Raw<T> &r, float (&v)[OCT])
     for (int k = 0; k < OCT; ++k) v[k] = raw_float(r, k);
 }
 
-template <typename T>
+template <bool STREAM = false, typename T>
 __device__ __forceinline__ void load_oct(const T *row, int32_t oct, const Cols &c, float (&v)[OCT])
 {
     Raw<T> r;
-    load_raw(row, oct, c, r);
+    load_raw<STREAM>(row, oct, c, r);
     settle(r, oct, c);
     raw_floats(r, v);
 }
 
-template <typename T>
+template <bool STREAM = false, typename T>
 __device__ __forceinline__ void store_oct(T *p, int valid, const float (&v)[OCT])
 {
     if (valid >= OCT) {
         Pack<T, OCT> w;
 #pragma unroll
         for (int k = 0; k < OCT; ++k) w.v[k] = from_float<T>(v[k]);
-        __builtin_memcpy(p, &w, sizeof w);
+        put_bytes<STREAM, sizeof w>(p, &w);
     } else {
 #pragma unroll
         for (int k = 0; k < OCT; ++k)
@@ -162,7 +194,7 @@ __device__ __forceinline__ float of_four(float x)
 // here hold the octets 4j .. 4j + 3 of one row as far as it has them.  An octet of fp32
 // is two 16-byte stores; the four lanes first exchange halves, so that each of the
 // stores covers 64 consecutive bytes of four lanes and not every other 16.
-template <typename T>
+template <bool STREAM = false, typename T>
 __device__ __forceinline__ void put_row_oct(T *row, int32_t oct, int32_t dim, bool fours,
                                             const float (&v)[OCT])
 {
@@ -178,13 +210,13 @@ __device__ __forceinline__ void put_row_oct(T *row, int32_t oct, int32_t dim, bo
                 b.v[k] = odd ? b1 : b0;
             }
             T *p = row + (int64_t)(oct & ~3) * OCT + (threadIdx.x & 3) * 4;
-            __builtin_memcpy(p, &a, sizeof a);
-            __builtin_memcpy(p + 16, &b, sizeof b);
+            put_bytes<STREAM, sizeof a>(p, &a);
+            put_bytes<STREAM, sizeof b>(p + 16, &b);
             return;
         }
     }
     const int left = dim - oct * OCT;
-    store_oct(row + (int64_t)oct * OCT, left < OCT ? left : OCT, v);
+    store_oct<STREAM>(row + (int64_t)oct * OCT, left < OCT ? left : OCT, v);
 }
 
 // ---------------------------------------------------------------- dropout
@@ -286,19 +318,21 @@ __global__ void __launch_bounds__(BLOCK) k_octets(Op op, Split s)
         op.first(row[k], g[k]);
     }
 #pragma unroll
-    for (int k = 0; k < U; ++k) op.load(row[k], at[k], g[k]);
+    for (int k = 0; k < U; ++k) op.template load<(U > 1)>(row[k], at[k], g[k]);
 #pragma unroll
     for (int k = 0; k < U; ++k)
-        if (on[k]) op.store(row[k], at[k], s.span % 4 == 0, g[k]);
+        if (on[k]) op.template store<(U > 1)>(row[k], at[k], s.span % 4 == 0, g[k]);
 }
 
-// With fewer octets than fill the card four times over, one octet per thread.
-constexpr int64_t OCTETS_FILL = 4ll * 256 * 2048;
+// Four octets per thread, outputs (and inputs that are read once) past the caches, where
+// there are octets for that: 32 MB of 16-bit values, what the L2s hold together.  Below, one
+// octet per thread, and the outputs stay near for the next kernel.
+constexpr int64_t OCTETS_DEEP = 1 << 21;
 template <class Op>
 inline hipError_t run_octets(const Op &op, int64_t n, int64_t dim, hipStream_t st)
 {
     const int64_t width = (dim + OCT - 1) / OCT;
-    const bool deep = n * width >= OCTETS_FILL;
+    const bool deep = n * width >= OCTETS_DEEP;
     const Split s = split_rows(n, width, deep ? 4 * BLOCK : BLOCK);
     const int64_t blocks = split_blocks(s);
     if (blocks <= 0) return hipSuccess;
