@@ -126,34 +126,51 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
         landed();
     }
 
+    // Out through LDS, 32 rows at a time: a lane then has consecutive outputs of a row, 16
+    // bytes of them, and a wave's store whole rows of its tile.
+    constexpr int EP = 16 / (int)sizeof(TO);   // outputs per lane and store
+    constexpr int LPR = WN / EP;               // lanes per row
+    constexpr int STRIDE = WN * 4 + 16;
+    static_assert(NW * 32 * STRIDE <= (int)sizeof sm && WAVE % LPR == 0, "staging fits the buffers");
+    int8_t *stage = &sm[0][0] + wave * 32 * STRIDE;
     TO *out = (TO *)a.out;
+    const int64_t n = n0 + wn + lane % LPR * EP;
+    float ws[EP];
+#pragma unroll
+    for (int c = 0; c < EP; ++c) ws[c] = a.ws[n + c < a.n ? n + c : a.n - 1];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + wm + i * 32 + lane % 32;
-        if (m >= a.m) continue;
-        const float xs = a.xs[m];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
+        for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int64_t n = n0 + wn + j * 32 + q * 8 + lane / 32 * 4;
-                TO *p = out + m * a.out_ld + n;
-                if (n + 4 <= a.n) {
-                    Pack<float, 4> ws;
-                    __builtin_memcpy(&ws, a.ws + n, sizeof ws);
-                    Pack<TO, 4> o;
+                const v4i v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2],
+                               acc[i][j][q * 4 + 3]};
+                *(v4i *)(stage + lane % 32 * STRIDE + (j * 32 + q * 8 + lane / 32 * 4) * 4) = v;
+            }
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        o.v[c] = from_float<TO>((float)acc[i][j][q * 4 + c] * xs * ws.v[c]);
-                    __builtin_memcpy(p, &o, sizeof o);
-                } else {
+        for (int r0 = 0; r0 < 32; r0 += WAVE / LPR) {
+            const int r = r0 + lane / LPR;
+            const int64_t m = m0 + wm + i * 32 + r;
+            int v[EP];
+            __builtin_memcpy(v, __builtin_assume_aligned(stage + r * STRIDE + lane % LPR * EP * 4, 16),
+                             sizeof v);
+            if (m >= a.m || n >= a.n) continue;
+            const float xs = a.xs[m];
+            Pack<TO, EP> o;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (n + c < a.n)
-                            p[c] = from_float<TO>((float)acc[i][j][q * 4 + c] * xs * a.ws[n + c]);
-                }
+            for (int c = 0; c < EP; ++c) o.v[c] = from_float<TO>((float)v[c] * xs * ws[c]);
+            TO *p = out + m * a.out_ld + n;
+            if (n + EP <= a.n) {
+                __builtin_memcpy(p, &o, sizeof o);
+            } else {
+#pragma unroll
+                for (int c = 0; c < EP; ++c)
+                    if (n + c < a.n) p[c] = o.v[c];
             }
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
