@@ -11,7 +11,8 @@ namespace sp {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
 
-constexpr int KT = 128;     // bytes of a row in one step
+constexpr int KT = 64;      // bytes of a row in one step
+constexpr int STAGES = 4;   // steps that LDS holds
 constexpr int CHUNK = 16;   // bytes of one access
 
 __device__ __forceinline__ void to_lds(const int8_t *src, int8_t *dst)
@@ -39,47 +40,83 @@ __device__ __forceinline__ v4i guarded_chunk(const int8_t *row, int32_t at, int3
 // ---------------------------------------------------------------- tiles
 //
 // A block computes BM x BN outputs, each wave WM x WN of them in 32 x 32 pieces, over
-// steps of 128 bytes of k, with two buffers in LDS: the rows of the next step arrive
-// straight in LDS while this one is multiplied.  A row's eight chunks of a step are
-// rotated among themselves by its number (chunk c of row r sits at c ^ (r >> 1 & 7)),
-// so that the 16 lanes that LDS serves at a time, 16 rows of one chunk, fall on
-// different banks.  w is the left factor of the matrix instruction: its four
-// consecutive rows per lane are four consecutive outputs of a row.
+// steps of 64 bytes of k.  LDS holds four steps: the rows of the step three ahead are on
+// their way straight to LDS while one is multiplied, their loads issued one by one
+// between the matrix instructions (issued together they kept a wave from those for as long as the
+// multiplication takes).  A row's four chunks of a step are rotated among themselves by
+// its number (chunk c of row r sits at c ^ (r >> 2 & 3)), so that the 16 lanes that LDS
+// serves at a time, 16 rows of one chunk, fall on different banks.  w is the left
+// factor of the matrix instruction: its four consecutive rows per lane are four
+// consecutive outputs of a row.
 template <int BM, int BN, int WM, int WN, typename TO, bool ALIGNED>
 __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs a, int32_t tiles_n)
 {
     constexpr int NW = (BM / WM) * (BN / WN), NT = NW * WAVE;
     constexpr int TM = WM / 32, TN = WN / 32;
-    constexpr int LOADS = (BM + BN) * (KT / CHUNK) / NT;
-    static_assert(LOADS * NT == (BM + BN) * (KT / CHUNK) && BM % (NW * 8) == 0, "whole loads");
-    __shared__ __attribute__((aligned(16))) int8_t sm[2][(BM + BN) * KT];
+    constexpr int CPR = KT / CHUNK, RPL = WAVE / CPR;  // chunks per row, rows per load of a wave
+    constexpr int LOADS = (BM + BN) * CPR / NT;        // of a wave and step
+    static_assert(LOADS * NT == (BM + BN) * CPR && BM % (NW * RPL) == 0, "whole loads");
+    constexpr int BUF = (BM + BN) * KT;
+    __shared__ __attribute__((aligned(16))) int8_t sm[STAGES * BUF];
     const int wave = wave_id(), lane = lane_id();
     const int64_t m0 = (int64_t)(blockIdx.x / (uint32_t)tiles_n) * BM;
     const int64_t n0 = (int64_t)(blockIdx.x % (uint32_t)tiles_n) * BN;
     const int32_t steps = (a.k + KT - 1) / KT;
-    const int32_t last_chunk = (a.k - 1) / CHUNK * CHUNK;
 
-    const auto fetch = [&](int buf, int32_t step) {
+    // The scales this lane will need, now: at the end their latency, and the wait for earlier
+    // stores that comes with any load, took as long as the stores themselves.
+    constexpr int EP = 16 / (int)sizeof(TO);  // outputs per lane and store
+    constexpr int LPR = WN / EP;              // lanes per row
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const int64_t n = n0 + wn + lane % LPR * EP;
+    float xs[TM], ws[EP];
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int r = (i * NW + wave) * 8 + lane / 8;  // of the x rows, then the w rows
-            const bool is_x = i * NW * 8 < BM;
-            const int64_t last = is_x ? a.m - 1 : a.n - 1;
-            const int64_t at = is_x ? m0 + r : n0 + (r - BM);
-            const int8_t *row = is_x ? a.x + (at < last ? at : last) * a.x_ld
-                                     : a.w + (at < last ? at : last) * a.w_ld;
-            int32_t kb = step * KT + ((lane % 8) ^ (r >> 1 & 7)) * CHUNK;
-            int8_t *dst = &sm[buf][(i * NW + wave) * 8 * KT];
-            if (ALIGNED) {
-                kb = kb < last_chunk ? kb : last_chunk;
-                to_lds(row + kb, dst);
-            } else {
-                *(v4i *)(dst + lane * CHUNK) = guarded_chunk(row, kb, a.k);
-            }
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = m0 + wm + i * 32 + lane % 32;
+        xs[i] = a.xs[m < a.m ? m : a.m - 1];
+    }
+#pragma unroll
+    for (int c = 0; c < EP; ++c) ws[c] = a.ws[n + c < a.n ? n + c : a.n - 1];
+
+    // This lane's chunk of each load: a place relative to the tile's first row, which with
+    // whole chunks fits 32 bits (ALIGNED: strides below 2^23).
+    uint32_t place[LOADS];
+    const int my_row = wave * RPL + lane / CPR;
+    const int my_chunk = (lane % CPR) ^ (my_row >> 2 & (CPR - 1));  // (RPL rows keep the rotation)
+    static_assert(NW * RPL % 16 == 0, "a load's rows rotate as the first one's");
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const bool is_x = i * NW * RPL < BM;
+        const int64_t last = is_x ? a.m - 1 - m0 : a.n - 1 - n0;
+        const int64_t at = i * NW * RPL + my_row - (is_x ? 0 : BM);
+        place[i] = (uint32_t)(at < last ? at : last) * (uint32_t)(is_x ? a.x_ld : a.w_ld) +
+                   (uint32_t)(my_chunk * CHUNK);
+    }
+    const int8_t *xt = a.x + m0 * a.x_ld, *wt = a.w + n0 * a.w_ld;
+    // Load i of a step; chunks past the rows' last one take that one.
+    const auto fetch = [&](int32_t step, int i) {
+        const bool is_x = i * NW * RPL < BM;
+        int8_t *dst = sm + step % STAGES * BUF + (i * NW + wave) * RPL * KT;
+        const int32_t kb = step * KT + my_chunk * CHUNK;
+        if (ALIGNED) {
+            const int32_t last = (a.k - 1) / CHUNK * CHUNK;
+            const int32_t back = kb > last ? kb - last : 0;
+            to_lds((is_x ? xt : wt) + step * KT + (place[i] - (uint32_t)back), dst);
+        } else {
+            const int64_t last = is_x ? a.m - 1 - m0 : a.n - 1 - n0;
+            const int64_t at = i * NW * RPL + my_row - (is_x ? 0 : BM);
+            const int8_t *row = (is_x ? xt : wt) + (at < last ? at : last) * (is_x ? a.x_ld : a.w_ld);
+            *(v4i *)(dst + lane * CHUNK) = guarded_chunk(row, kb, a.k);
         }
     };
+    // Every wave's loads but its last `open` are in LDS, and every wave is done with the
+    // buffer that is filled next.
+    const auto landed = [](int open) {
+        if (open >= 2 * LOADS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
+        else if (open >= LOADS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
 
-    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
     v16i acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -88,82 +125,110 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
 
-    // the loads of a step are in LDS: every wave waits for its own, then for the others
-    const auto landed = [&] {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+    // Two sets of factors in registers: while one is multiplied the next arrives from LDS,
+    // also over the edge of a step.
+    constexpr int KS = KT / 32;
+    static_assert(KS == 2, "two sets");
+    v4i x[2][TM], w[2][TN];
+    const int8_t *xb = sm + (wm + lane % 32) * KT, *wb = sm + (BM + wn + lane % 32) * KT;
+    const auto read = [&](int32_t step, int ks, int i) {  // factor i of a set: x's, then w's
+        const int at = step % STAGES * BUF + ((ks * 2 + lane / 32) ^ (lane >> 2 & (CPR - 1))) * CHUNK;
+        if (i < TM) x[ks][i] = *(const v4i *)(xb + i * 32 * KT + at);
+        else w[ks][i - TM] = *(const v4i *)(wb + (i - TM) * 32 * KT + at);
     };
-    fetch(0, 0);
-    landed();
-    for (int32_t s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fetch((s + 1) & 1, s + 1);
-        const int8_t *xb = &sm[s & 1][(wm + lane % 32) * KT];
-        const int8_t *wb = &sm[s & 1][(BM + wn + lane % 32) * KT];
+    // Set ks multiplied.  Between the matrix instructions: the other set's reads (of step
+    // `next`), and the loads of step `ahead`; -1: none.
+    const auto multiply = [&](int ks, int32_t next, int32_t ahead) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < KT / 32; ++ks) {
-            const int at = ((ks * 2 + lane / 32) ^ (lane >> 1 & 7)) * CHUNK;
-            v4i x[TM], w[TN];
+        for (int t = 0; t < TM * TN; ++t) {
+            acc[t / TN][t % TN] = __builtin_amdgcn_mfma_i32_32x32x32_i8(
+                w[ks][t % TN], x[ks][t / TN], acc[t / TN][t % TN], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (next >= 0) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i) x[i] = *(const v4i *)(xb + i * 32 * KT + at);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) w[j] = *(const v4i *)(wb + j * 32 * KT + at);
-            const int32_t left = a.k - s * KT - (ks * 2 + lane / 32) * CHUNK;
-            if (left < CHUNK) {  // what lies past the rows' end counts nothing
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int32_t b = left - 4 * q;
-                    const int mask = b >= 4 ? -1 : b <= 0 ? 0 : (int)((1u << (8 * b)) - 1);
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) x[i][q] &= mask;
-                }
+                for (int i = 0; i < TM + TN; ++i)
+                    if (i * (TM * TN) / (TM + TN) == t) read(next, ks ^ 1, i);
             }
+            if (ahead >= 0) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[j], x[i], acc[i][j], 0, 0, 0);
+                for (int i = 0; i < LOADS; ++i)
+                    if (i * (TM * TN) / LOADS == t) fetch(ahead, i);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        landed();
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+        if (s < steps) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) fetch(s, i);
+        }
+    landed((steps < STAGES - 1 ? steps - 1 : STAGES - 2) * LOADS);
+#pragma unroll
+    for (int i = 0; i < TM + TN; ++i) read(0, 0, i);
+    int32_t s = 0;
+    for (; s + STAGES - 1 < steps; ++s) {
+        multiply(0, s, s + STAGES - 1);
+        landed(2 * LOADS);
+        multiply(1, s + 1, -1);
     }
+    for (; s + 1 < steps; ++s) {
+        multiply(0, s, -1);
+        landed(s + 2 < steps ? LOADS : 0);
+        multiply(1, s + 1, -1);
+    }
+#pragma unroll
+    for (int i = 0; i < TM + TN; ++i) read(s, 1, i);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {  // the last step: what lies past the rows' end counts nothing
+        const int32_t left = a.k - s * KT - (ks * 2 + lane / 32) * CHUNK;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int32_t b = left - 4 * q;
+            const int mask = b >= 4 ? -1 : b <= 0 ? 0 : (int)((1u << (8 * b)) - 1);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) x[ks][i][q] &= mask;
+        }
+        multiply(ks, -1, -1);
+    }
+    __syncthreads();
 
     // Out through LDS, 32 rows at a time: a lane then has consecutive outputs of a row, 16
     // bytes of them, and a wave's store whole rows of its tile.
-    constexpr int EP = 16 / (int)sizeof(TO);   // outputs per lane and store
-    constexpr int LPR = WN / EP;               // lanes per row
     constexpr int STRIDE = WN * 4 + 16;
     static_assert(NW * 32 * STRIDE <= (int)sizeof sm && WAVE % LPR == 0, "staging fits the buffers");
-    int8_t *stage = &sm[0][0] + wave * 32 * STRIDE;
-    TO *out = (TO *)a.out;
-    const int64_t n = n0 + wn + lane % LPR * EP;
-    float ws[EP];
-#pragma unroll
-    for (int c = 0; c < EP; ++c) ws[c] = a.ws[n + c < a.n ? n + c : a.n - 1];
+    int8_t *stage = sm + wave * 32 * STRIDE;
+    TO *out = (TO *)a.out + (m0 + wm + lane / LPR) * a.out_ld + n;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const v4i v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2],
-                               acc[i][j][q * 4 + 3]};
-                *(v4i *)(stage + lane % 32 * STRIDE + (j * 32 + q * 8 + lane / 32 * 4) * 4) = v;
+                Pack<float, 4> v;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v.v[c] = (float)acc[i][j][q * 4 + c] * xs[i];
+                __builtin_memcpy(
+                    __builtin_assume_aligned(
+                        stage + lane % 32 * STRIDE + (j * 32 + q * 8 + lane / 32 * 4) * 4, 16),
+                    &v, sizeof v);
             }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int r0 = 0; r0 < 32; r0 += WAVE / LPR) {
-            const int r = r0 + lane / LPR;
-            const int64_t m = m0 + wm + i * 32 + r;
-            int v[EP];
-            __builtin_memcpy(v, __builtin_assume_aligned(stage + r * STRIDE + lane % LPR * EP * 4, 16),
+            Pack<float, EP> v;
+            __builtin_memcpy(&v, __builtin_assume_aligned(stage + (r0 + lane / LPR) * STRIDE +
+                                                              lane % LPR * EP * 4, 16),
                              sizeof v);
-            if (m >= a.m || n >= a.n) continue;
-            const float xs = a.xs[m];
             Pack<TO, EP> o;
 #pragma unroll
-            for (int c = 0; c < EP; ++c) o.v[c] = from_float<TO>((float)v[c] * xs * ws[c]);
-            TO *p = out + m * a.out_ld + n;
+            for (int c = 0; c < EP; ++c) o.v[c] = from_float<TO>(v.v[c] * ws[c]);
+            TO *p = out + (int64_t)(i * 32 + r0) * a.out_ld;
+            if (m0 + wm + i * 32 + r0 + lane / LPR >= a.m) continue;
             if (n + EP <= a.n) {
-                __builtin_memcpy(p, &o, sizeof o);
+                if (a.stream) put_bytes<true, sizeof o>(p, &o);
+                else put_bytes<false, sizeof o>(p, &o);
             } else {
 #pragma unroll
                 for (int c = 0; c < EP; ++c)
@@ -179,7 +244,9 @@ int64_t product_workspace(int64_t, int64_t, int64_t) { return 0; }
 template <typename TO>
 static hipError_t product_as(const ProductArgs &a, hipStream_t s)
 {
-    const bool aligned = ((uintptr_t)a.x | (uintptr_t)a.w | (uint64_t)a.x_ld | (uint64_t)a.w_ld) % CHUNK == 0;
+    const bool aligned =
+        ((uintptr_t)a.x | (uintptr_t)a.w | (uint64_t)a.x_ld | (uint64_t)a.w_ld) % CHUNK == 0 &&
+        a.x_ld < 1 << 23 && a.w_ld < 1 << 23;
     constexpr int BM = 128, BN = 128;
     const int64_t tm = (a.m + BM - 1) / BM, tn = (a.n + BN - 1) / BN;
     if (tm * tn > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
@@ -188,8 +255,10 @@ static hipError_t product_as(const ProductArgs &a, hipStream_t s)
                    : launch(k_product<BM, BN, 64, 64, TO, false>, grid, block, s, a, (int32_t)tn);
 }
 
-hipError_t run_product(const ProductArgs &a, hipStream_t s)
+hipError_t run_product(const ProductArgs &given, hipStream_t s)
 {
+    ProductArgs a = given;
+    a.stream = a.m * a.n >= 1 << 24;  // as k_octets: 32 MB of 16-bit outputs
     return with_type(a.out_type, [&](auto to) { return product_as<decltype(to)>(a, s); });
 }
 
