@@ -4,6 +4,9 @@
 //
 // The sums are exact in 32 bits (k <= 131071); each is rounded to fp32 once, scaled in
 // fp32 and rounded once to the output's type.
+#include <cmath>
+#include <type_traits>
+
 #include "sp_rows.h"
 
 namespace sp {
@@ -49,7 +52,7 @@ __device__ __forceinline__ v4i guarded_chunk(const int8_t *row, int32_t at, int3
 // factor of the matrix instruction: its four consecutive rows per lane are four
 // consecutive outputs of a row.
 template <int BM, int BN, int WM, int WN, typename TO, bool ALIGNED>
-__global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs a, int32_t tiles_n)
+__global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs a, int32_t tiles_n, int32_t per_split)
 {
     constexpr int NW = (BM / WM) * (BN / WN), NT = NW * WAVE;
     constexpr int TM = WM / 32, TN = WN / 32;
@@ -61,7 +64,9 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
     const int wave = wave_id(), lane = lane_id();
     const int64_t m0 = (int64_t)(blockIdx.x / (uint32_t)tiles_n) * BM;
     const int64_t n0 = (int64_t)(blockIdx.x % (uint32_t)tiles_n) * BN;
-    const int32_t steps = (a.k + KT - 1) / KT;
+    constexpr bool PARTIAL = std::is_same<TO, int32_t>::value;  // sums of a part of k
+    const int32_t first = (int32_t)blockIdx.y * per_split;
+    const int32_t all = (a.k + KT - 1) / KT, steps = first + per_split < all ? first + per_split : all;
 
     // The scales this lane will need, now: at the end their latency, and the wait for earlier
     // stores that comes with any load, took as long as the stores themselves.
@@ -73,10 +78,10 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int64_t m = m0 + wm + i * 32 + lane % 32;
-        xs[i] = a.xs[m < a.m ? m : a.m - 1];
+        xs[i] = PARTIAL ? 1.f : a.xs[m < a.m ? m : a.m - 1];
     }
 #pragma unroll
-    for (int c = 0; c < EP; ++c) ws[c] = a.ws[n + c < a.n ? n + c : a.n - 1];
+    for (int c = 0; c < EP; ++c) ws[c] = PARTIAL ? 1.f : a.ws[n + c < a.n ? n + c : a.n - 1];
 
     // This lane's chunk of each load: a place relative to the tile's first row, which with
     // whole chunks fits 32 bits (ALIGNED: strides below 2^23).
@@ -160,14 +165,14 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
     };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s)
-        if (s < steps) {
+        if (first + s < steps) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) fetch(s, i);
+            for (int i = 0; i < LOADS; ++i) fetch(first + s, i);
         }
-    landed((steps < STAGES - 1 ? steps - 1 : STAGES - 2) * LOADS);
+    landed((steps - first < STAGES - 1 ? steps - first - 1 : STAGES - 2) * LOADS);
 #pragma unroll
-    for (int i = 0; i < TM + TN; ++i) read(0, 0, i);
-    int32_t s = 0;
+    for (int i = 0; i < TM + TN; ++i) read(first, 0, i);
+    int32_t s = first;
     for (; s + STAGES - 1 < steps; ++s) {
         multiply(0, s, s + STAGES - 1);
         landed(2 * LOADS);
@@ -199,16 +204,18 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
     constexpr int STRIDE = WN * 4 + 16;
     static_assert(NW * 32 * STRIDE <= (int)sizeof sm && WAVE % LPR == 0, "staging fits the buffers");
     int8_t *stage = sm + wave * 32 * STRIDE;
-    TO *out = (TO *)a.out + (m0 + wm + lane / LPR) * a.out_ld + n;
+    using Held = typename std::conditional<PARTIAL, int32_t, float>::type;
+    TO *out = (PARTIAL ? (TO *)a.work + (int64_t)blockIdx.y * a.m * a.n : (TO *)a.out) + (m0 + wm + lane / LPR) * a.out_ld + n;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                Pack<float, 4> v;
+                Pack<Held, 4> v;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v.v[c] = (float)acc[i][j][q * 4 + c] * xs[i];
+                for (int c = 0; c < 4; ++c)
+                    v.v[c] = PARTIAL ? (Held)acc[i][j][q * 4 + c] : (Held)((float)acc[i][j][q * 4 + c] * xs[i]);
                 __builtin_memcpy(
                     __builtin_assume_aligned(
                         stage + lane % 32 * STRIDE + (j * 32 + q * 8 + lane / 32 * 4) * 4, 16),
@@ -217,13 +224,13 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int r0 = 0; r0 < 32; r0 += WAVE / LPR) {
-            Pack<float, EP> v;
+            Pack<Held, EP> v;
             __builtin_memcpy(&v, __builtin_assume_aligned(stage + (r0 + lane / LPR) * STRIDE +
                                                               lane % LPR * EP * 4, 16),
                              sizeof v);
             Pack<TO, EP> o;
 #pragma unroll
-            for (int c = 0; c < EP; ++c) o.v[c] = from_float<TO>(v.v[c] * ws[c]);
+            for (int c = 0; c < EP; ++c) o.v[c] = PARTIAL ? (TO)v.v[c] : from_float<TO>(v.v[c] * ws[c]);
             TO *p = out + (int64_t)(i * 32 + r0) * a.out_ld;
             if (m0 + wm + i * 32 + r0 + lane / LPR >= a.m) continue;
             if (n + EP <= a.n) {
@@ -239,27 +246,126 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
     }
 }
 
-int64_t product_workspace(int64_t, int64_t, int64_t) { return 0; }
-
+// The parts of a split sum added up, scaled and rounded: four outputs per thread.
 template <typename TO>
-static hipError_t product_as(const ProductArgs &a, hipStream_t s)
+__global__ void __launch_bounds__(BLOCK) k_product_join(ProductArgs a, int32_t splits)
+{
+    const int64_t total = a.m * a.n, i0 = ((int64_t)blockIdx.x * BLOCK + threadIdx.x) * 4;
+    if (i0 >= total) return;
+    const int32_t *part = (const int32_t *)a.work + i0;
+    int v[4] = {0, 0, 0, 0};
+    const int valid = total - i0 < 4 ? (int)(total - i0) : 4;
+    if (valid == 4) {
+#pragma unroll 4
+        for (int32_t s = 0; s < splits; ++s) {
+            Pack<int, 4> p;
+            __builtin_memcpy(&p, part + s * total, sizeof p);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] += p.v[c];
+        }
+    } else {
+        for (int32_t s = 0; s < splits; ++s)
+            for (int c = 0; c < valid; ++c) v[c] += part[s * total + c];
+    }
+    int64_t m = i0 / a.n, n = i0 - m * a.n;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        if (c < valid) ((TO *)a.out)[m * a.out_ld + n] = from_float<TO>((float)v[c] * a.xs[m] * a.ws[n]);
+        if (++n == a.n) n = 0, ++m;
+    }
+}
+
+// ---------------------------------------------------------------- host
+
+// How a product is cut: into tiles, and parts of k where the tiles are few.  The estimate,
+// in us, for what each CU has to do one after the other: a tile's fixed time (first loads,
+// outputs) and its steps of k, with the card mostly idle or busy, and for parts a second
+// launch and their traffic.  Measured on both sides of the lines that it draws (us):
+//                        256x256  128x128  64x128  64x64  32x64   in parts
+//   8192 x 8192 x 8192       471      662
+//   777 x 10001 x 1000        22       27      32     34     50
+//   2048 x 2048 x 2048        28       18      19     22     27
+//   1500 x 700 x 3000         35       21      15     17     19   19 (2 of 128x128)
+//   256 x 4096 x 4096         42       25      19     15     15   19 (2 of 64x64)
+//   128 x 8192 x 8192         84       50      44     36     41   27 (4 of 128x128)
+//   64 x 4096 x 4096                   25      18     14     13   11 (4 of 64x64)
+//   33 x 2000 x 512                     7       6      5      5    7 (2 of 32x64)
+//   424 x 222 x 3424          40       23      16     12     12    9 (4 of 32x64)
+struct Cut {
+    int32_t tile, splits;
+};
+static Cut cut_product(int64_t m, int64_t n, int64_t k)
+{
+    constexpr struct {
+        int bm, bn;
+        double idle, busy, fixed;
+    } T[] = {{256, 256, 0.56, 0.86, 7.3}, {128, 128, 0.33, 0.31, 1.8}, {64, 128, 0.22, 0.24, 1.0},
+             {64, 64, 0.165, 0.19, 0.6}, {32, 64, 0.155, 0.16, 0.5}};
+    const int64_t steps = (k + KT - 1) / KT;
+    Cut best{1, 1};
+    double least = 1e300;
+    for (int t = 0; t < 5; ++t) {
+        const double tiles = (double)((m + T[t].bm - 1) / T[t].bm) * (double)((n + T[t].bn - 1) / T[t].bn);
+        for (int sp = 1; sp <= 16; sp *= 2) {
+            if (sp > 1 && (steps < 4 * sp || tiles * sp > 1024)) break;
+            const double blocks = tiles * sp, step = blocks <= 192 ? T[t].idle : T[t].busy;
+            double us = std::ceil(blocks / 256) * (T[t].fixed + step * (double)((steps + sp - 1) / sp));
+            if (sp > 1) us += 3.0 + (double)m * (double)n * 4.0 * (2 * sp) / 4e6;
+            if (us < least) least = us, best = Cut{t, sp};
+        }
+    }
+    return best;
+}
+
+int64_t product_workspace(int64_t m, int64_t n, int64_t k)
+{
+    if (m == 0 || n == 0) return 0;
+    const Cut c = cut_product(m, n, k);
+    return c.splits > 1 ? m * n * 4 * c.splits : 0;
+}
+
+template <int BM, int BN, int WM, int WN, typename TO>
+static hipError_t run_tiles(const ProductArgs &a, int32_t splits, hipStream_t s)
 {
     const bool aligned =
         ((uintptr_t)a.x | (uintptr_t)a.w | (uint64_t)a.x_ld | (uint64_t)a.w_ld) % CHUNK == 0 &&
         a.x_ld < 1 << 23 && a.w_ld < 1 << 23;
-    constexpr int BM = 128, BN = 128;
     const int64_t tm = (a.m + BM - 1) / BM, tn = (a.n + BN - 1) / BN;
     if (tm * tn > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)(tm * tn)), block(4 * WAVE);
-    return aligned ? launch(k_product<BM, BN, 64, 64, TO, true>, grid, block, s, a, (int32_t)tn)
-                   : launch(k_product<BM, BN, 64, 64, TO, false>, grid, block, s, a, (int32_t)tn);
+    const int32_t steps = (a.k + KT - 1) / KT, per = (steps + splits - 1) / splits;
+    const dim3 grid((unsigned)(tm * tn), (unsigned)((steps + per - 1) / per)), block(BM / WM * (BN / WN) * WAVE);
+    return aligned ? launch(k_product<BM, BN, WM, WN, TO, true>, grid, block, s, a, (int32_t)tn, per)
+                   : launch(k_product<BM, BN, WM, WN, TO, false>, grid, block, s, a, (int32_t)tn, per);
+}
+
+template <typename TO>
+static hipError_t run_cut(const ProductArgs &a, const Cut &c, hipStream_t s)
+{
+    return c.tile == 0   ? run_tiles<256, 256, 128, 64, TO>(a, c.splits, s)
+           : c.tile == 1 ? run_tiles<128, 128, 64, 64, TO>(a, c.splits, s)
+           : c.tile == 2 ? run_tiles<64, 128, 32, 64, TO>(a, c.splits, s)
+           : c.tile == 3 ? run_tiles<64, 64, 32, 32, TO>(a, c.splits, s)
+                         : run_tiles<32, 64, 32, 32, TO>(a, c.splits, s);
 }
 
 hipError_t run_product(const ProductArgs &given, hipStream_t s)
 {
     ProductArgs a = given;
     a.stream = a.m * a.n >= 1 << 24;  // as k_octets: 32 MB of 16-bit outputs
-    return with_type(a.out_type, [&](auto to) { return product_as<decltype(to)>(a, s); });
+    const Cut c = cut_product(a.m, a.n, a.k);
+    return with_type(a.out_type, [&](auto to) {
+        using TO = decltype(to);
+        if (c.splits == 1) return run_cut<TO>(a, c, s);
+        ProductArgs p = a;
+        p.out_ld = a.n;
+        p.stream = false;
+        hipError_t r = run_cut<int32_t>(p, c, s);
+        if (r != hipSuccess) return r;
+        const int32_t steps = (a.k + KT - 1) / KT, per = (steps + c.splits - 1) / c.splits;
+        const int64_t blocks = (a.m * a.n + 4 * BLOCK - 1) / (4 * BLOCK);
+        if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+        return launch(k_product_join<TO>, dim3((unsigned)blocks), dim3(BLOCK), s, a, (steps + per - 1) / per);
+    });
 }
 
 }  // namespace sp

@@ -68,17 +68,14 @@ __device__ __forceinline__ void put_oct(const GradArgs &a, int64_t row, int32_t 
 
 // ---------------------------------------------------------------- few positions
 
-// Block b < sums: one position and slab of columns.  Every wave looks for the
-// position's token among all tokens, 64 at a time; the token's first position adds up
-// its rows (each wave those of every fourth group of 64 positions, joined in LDS).  The
-// other blocks write zeros to their rows without a token.
 constexpr int FILL_UNITS = 4096;  // 16-byte pieces of rows that one block of a fill looks after
 template <typename TO>
 constexpr int FILL_COLS = 16 / (int)sizeof(TO);
 
-// Zeros to the pieces of block b's rows that `used` does not name.  Pieces of 16 bytes,
-// so that a wave's store is one stretch: with octets, 32 bytes of fp32 per lane in two
-// stores, a fill of 1.07 GB ran at 4.3 TB/s.
+// Zeros to the pieces of block b's rows that `used` does not name.  Pieces of 16 bytes at
+// multiples of 16, so that a wave's store is one aligned stretch (with octets, 32
+// bytes of fp32 per lane in two stores, a fill of 1.07 GB ran at 4.3 TB/s).  Where
+// rows start elsewhere, their first and last pieces are parts of one.
 template <typename TO, int NT>
 __device__ __forceinline__ void fill_zeros(const GradArgs &a, const Split &fill, int64_t b,
                                            int64_t row0, const uint8_t *used)
@@ -92,14 +89,28 @@ __device__ __forceinline__ void fill_zeros(const GradArgs &a, const Split &fill,
         int64_t row;
         int32_t at;
         if (!split_at(fill, b, k * NT + (int)threadIdx.x, row, at) || used[row - row0]) continue;
-        TO *p = (TO *)a.out + row * a.out_ld + at * C;
-        if (a.dim - at * C >= C) {
-            __builtin_memcpy(p, &z, sizeof z);
+        TO *p = (TO *)a.out + row * a.out_ld;
+        const int32_t col = at * C - (int32_t)((uintptr_t)p % 16 / sizeof(TO));
+        if (col >= 0 && col + C <= a.dim) {
+            __builtin_memcpy(__builtin_assume_aligned(p + col, 16), &z, sizeof z);
         } else {
-            for (int k = 0; k < a.dim - at * C; ++k) p[k] = z.v[0];
+            for (int q = 0; q < C; ++q)
+                if (col + q >= 0 && col + q < a.dim) p[col + q] = z.v[0];
         }
     }
 }
+template <typename TO>
+static int64_t fill_pieces(const GradArgs &a)
+{
+    constexpr int C = FILL_COLS<TO>;
+    const bool aligned = ((uintptr_t)a.out | (uint64_t)a.out_ld * sizeof(TO)) % 16 == 0;
+    return ((int64_t)a.dim + C - 1) / C + !aligned;
+}
+
+// Block b < sums: one position and slab of columns.  Every wave looks for the
+// position's token among all tokens, 64 at a time; the token's first position adds up
+// its rows (each wave those of every fourth group of 64 positions, joined in LDS).  The
+// other blocks write zeros to their rows without a token.
 template <typename TI, typename TO, typename IX>
 __global__ void __launch_bounds__(BLOCK) k_grad_direct(GradArgs a, int32_t slabs, int64_t sums,
                                                        Split fill)
@@ -173,32 +184,41 @@ __global__ void __launch_bounds__(BLOCK) k_grad_direct(GradArgs a, int32_t slabs
 
 // ---------------------------------------------------------------- places by counting
 
-// 64 positions per block, one per lane; 16 waves count over a sixteenth of the keys each.
+// RANK_POS positions per block; each of its 64 groups of RANK_POS lanes counts, for all of
+// them, over a 64th of the keys, four at a time from LDS.  A key before the block's own
+// positions counts where it is at most theirs, one after them where it is less; among
+// the block's own positions equal keys are counted at the end.
 constexpr int RANK_NT = 1024;
+constexpr int RANK_POS = 16;
+constexpr int RANK_PARTS = RANK_NT / RANK_POS;
 template <typename IX>
 __global__ void __launch_bounds__(RANK_NT) k_grad_rank(const IX *tokens, int32_t n, int64_t rows,
                                                        uint64_t *out)
 {
-    __shared__ uint32_t keys[RANK_MAX];
-    __shared__ uint32_t count[RANK_NT / WAVE][WAVE];
-    for (int i = threadIdx.x; i < n; i += RANK_NT) keys[i] = key_at(tokens, i, rows);
+    __shared__ __attribute__((aligned(16))) uint32_t keys[RANK_MAX + RANK_POS];
+    __shared__ uint32_t count[RANK_PARTS][RANK_POS];
+    const int own = (int)blockIdx.x * RANK_POS;
+    const int padded = (n + RANK_POS - 1) / RANK_POS * RANK_POS;
+    for (int i = threadIdx.x; i < padded; i += RANK_NT)
+        keys[i] = i < n ? key_at(tokens, i, rows) : 0xFFFFFFFFu;  // counts nowhere
     __syncthreads();
-    const int i = (int)blockIdx.x * WAVE + lane_id();
-    const uint32_t k = keys[i < n ? i : 0];
-    const int per = (n + RANK_NT / WAVE - 1) / (RANK_NT / WAVE);
-    const int j0 = wave_id() * per, j1 = j0 + per < n ? j0 + per : n;
+    const int pos = (int)threadIdx.x % RANK_POS, group = (int)threadIdx.x / RANK_POS;
+    const uint32_t k = keys[own + pos];
     uint32_t c = 0;
-    int j = j0;
-    for (; j < j1 && j < (int)blockIdx.x * WAVE; ++j) c += keys[j] <= k;  // before the block's own
-    for (; j < j1 && j < (int)blockIdx.x * WAVE + WAVE; ++j) c += keys[j] < k || (keys[j] == k && j < i);
-    for (; j < j1; ++j) c += keys[j] < k;
-    count[wave_id()][lane_id()] = c;
+#pragma unroll 4
+    for (int j = group * 4; j < padded; j += RANK_PARTS * 4) {
+        const uint4 x = *(const uint4 *)(keys + j);
+        const uint32_t below = k + (j < own);
+        c += (x.x < below) + (x.y < below) + (x.z < below) + (x.w < below);
+    }
+    if (group < pos) c += keys[own + group] == k;  // (RANK_PARTS >= RANK_POS)
+    count[group][pos] = c;
     __syncthreads();
-    if (threadIdx.x < WAVE && i < n) {
+    if (threadIdx.x < RANK_POS && own + pos < n) {
         uint32_t at = 0;
-#pragma unroll
-        for (int w = 0; w < RANK_NT / WAVE; ++w) at += count[w][threadIdx.x];
-        out[at] = (uint64_t)k << 32 | (uint32_t)i;
+#pragma unroll 8
+        for (int w = 0; w < RANK_PARTS; ++w) at += count[w][pos];
+        out[at] = (uint64_t)k << 32 | (uint32_t)(own + pos);
     }
 }
 
@@ -636,7 +656,7 @@ static hipError_t sort_tokens(const GradArgs &a, const GradWs &w, uint64_t **sor
     uint64_t *e0 = (uint64_t *)(a.ws + w.e0), *e1 = (uint64_t *)(a.ws + w.e1);
     if (a.n <= RANK_MAX) {
         *sorted = e0;
-        return launch(k_grad_rank<IX>, dim3((unsigned)((a.n + WAVE - 1) / WAVE)), dim3(RANK_NT), s,
+        return launch(k_grad_rank<IX>, dim3((unsigned)((a.n + RANK_POS - 1) / RANK_POS)), dim3(RANK_NT), s,
                       (const IX *)a.tokens, (int32_t)a.n, a.rows, e0);
     }
     int bits = 1;
@@ -669,8 +689,7 @@ static hipError_t sort_tokens(const GradArgs &a, const GradWs &w, uint64_t **sor
 template <typename TI, typename TO, typename IX>
 static hipError_t run_grad_as(const GradArgs &a, hipStream_t s)
 {
-    const int64_t width = ((int64_t)a.dim + FILL_COLS<TO> - 1) / FILL_COLS<TO>;
-    const Split fill = split_rows(a.add ? 0 : a.rows, width, FILL_UNITS);
+    const Split fill = split_rows(a.add ? 0 : a.rows, fill_pieces<TO>(a), FILL_UNITS);
     const int64_t fills = split_blocks(fill);
     if (a.n <= DIRECT_MAX) {
         const int32_t slabs = (int32_t)((a.dim + SLAB - 1) / SLAB);
