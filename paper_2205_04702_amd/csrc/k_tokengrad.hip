@@ -41,11 +41,15 @@ template <typename TI>
 __device__ __forceinline__ void add_oct(const GradArgs &a, Raw<TI> &r, int64_t pos, int32_t oct,
                                         bool counts, float (&acc)[OCT])
 {
-    uint32_t keep = counts ? 0xFFu : 0u;
-    if (a.drop.drop) keep &= keep_oct(a.drop, (uint32_t)oct, (uint32_t)pos);  // the same for all
     settle(r, oct, cols_of(a.dim));
+    if (a.drop.drop) {  // the same for all
+        const Kept keep = keep_oct(a.drop, (uint32_t)oct, (uint32_t)pos);
 #pragma unroll
-    for (int k = 0; k < OCT; ++k) acc[k] += keep >> k & 1u ? raw_float(r, k) : 0.f;
+        for (int k = 0; k < OCT; ++k) acc[k] += counts && keep(a.drop, k) ? raw_float(r, k) : 0.f;
+    } else {
+#pragma unroll
+        for (int k = 0; k < OCT; ++k) acc[k] += counts ? raw_float(r, k) : 0.f;
+    }
 }
 
 // A finished sum goes to its row of the table gradient (a team's lanes together).
@@ -616,14 +620,15 @@ static int team_lanes(int32_t dim)
 }
 
 // Pieces of 4 to 32 entries per team: enough blocks for the card where there are few
-// entries, few cut runs where there are many.
+// entries, few cut runs where there are many.  Narrow rows have many teams in a block and
+// take 8 or 16 at least: a run goes from team to team in turn.
 static SumShape sum_shape(int64_t n, int32_t dim)
 {
     const int lpr = team_lanes(dim), teams = SUM_NT / lpr;
     SumShape s;
     s.slabs = (dim + lpr * OCT - 1) / (lpr * OCT);
-    int64_t per = n * s.slabs / ((int64_t)teams * 1024);
-    s.per = (int32_t)(per < 4 ? 4 : per > 32 ? 32 : per);
+    const int64_t per = n * s.slabs / ((int64_t)teams * 1024), least = lpr < 16 ? 64 / lpr : 4;
+    s.per = (int32_t)(per < least ? least : per > 32 ? 32 : per);
     s.chunks = (n + (int64_t)s.per * teams - 1) / ((int64_t)s.per * teams);
     s.part_ld = ((int64_t)dim + OCT - 1) / OCT * OCT;
     return s;

@@ -31,13 +31,14 @@ struct Lookup {
     template <bool STREAM>
     __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
     {
-        uint32_t keep = g.live ? 0xFFu : 0u;
-        if (DROP) keep &= keep_oct(drop, (uint32_t)oct, (uint32_t)row);
+        Kept keep;
+        if (DROP) keep = keep_oct(drop, (uint32_t)oct, (uint32_t)row);
         float v[OCT];
         settle(g.r, oct, cols_of(dim));
         raw_floats(g.r, v);
 #pragma unroll
-        for (int k = 0; k < OCT; ++k) v[k] = keep >> k & 1u ? v[k] * factor : 0.f;
+        for (int k = 0; k < OCT; ++k)
+            v[k] = g.live && (!DROP || keep(drop, k)) ? v[k] * factor : 0.f;
         put_row_oct<STREAM>(out + row * out_ld, oct, dim, fours, v);
     }
 };
@@ -94,7 +95,7 @@ struct Dropout {
     template <bool STREAM>
     __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
     {
-        const uint32_t keep = keep_oct(drop, (uint32_t)oct, (uint32_t)row);
+        const Kept keep = keep_oct(drop, (uint32_t)oct, (uint32_t)row);
         float v[OCT], r[OCT];
         settle(g.x, oct, cols_of(dim));
         raw_floats(g.x, v);
@@ -104,7 +105,7 @@ struct Dropout {
         }
 #pragma unroll
         for (int k = 0; k < OCT; ++k) {
-            v[k] = keep >> k & 1u ? v[k] * factor : 0.f;
+            v[k] = keep(drop, k) ? v[k] * factor : 0.f;
             if (RES) v[k] += r[k];
         }
         put_row_oct<STREAM>(out + row * out_ld, oct, dim, fours, v);

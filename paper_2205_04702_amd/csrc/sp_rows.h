@@ -233,27 +233,34 @@ struct Drop {
     uint32_t k0, k1, o0, o1, drop;  // drop 0: keep everything
 };
 
-__device__ __forceinline__ uint32_t keep_oct(const Drop &d, uint32_t oct, uint32_t row)
+struct Kept {
+    uint32_t w[4];
+    // whether column k (0 .. 7) of the octet is kept: the high halves compare as they lie
+    __device__ __forceinline__ bool operator()(const Drop &d, int k) const
+    {
+        return (k & 1 ? w[k / 2] : w[k / 2] << 16) >= d.drop << 16;
+    }
+};
+
+__device__ __forceinline__ uint32_t xor3(uint32_t x, uint32_t y, uint32_t z)
+{
+    return (uint32_t)__builtin_amdgcn_bitop3_b32((int)x, (int)y, (int)z, 0x96);
+}
+
+__device__ __forceinline__ Kept keep_oct(const Drop &d, uint32_t oct, uint32_t row)
 {
     uint32_t a = oct, b = row, c = d.o0, e = d.o1, k0 = d.k0, k1 = d.k1;
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t x = (uint64_t)a * 0xD2511F53u, y = (uint64_t)c * 0xCD9E8D57u;
-        a = (uint32_t)(y >> 32) ^ b ^ k0;
+        a = xor3((uint32_t)(y >> 32), b, k0);
         b = (uint32_t)y;
-        c = (uint32_t)(x >> 32) ^ e ^ k1;
+        c = xor3((uint32_t)(x >> 32), e, k1);
         e = (uint32_t)x;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    uint32_t keep = 0;
-    const uint32_t w[4] = {a, b, c, e};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        keep |= (uint32_t)((w[i] & 0xFFFFu) >= d.drop) << (2 * i);
-        keep |= (uint32_t)((w[i] >> 16) >= d.drop) << (2 * i + 1);
-    }
-    return keep;
+    return Kept{{a, b, c, e}};
 }
 
 // ---------------------------------------------------------------- rows over a grid
