@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(BLOCK) k_cache_write(CacheArgs a, Split s, int
 #pragma unroll
         for (int i = 0; i < OPL; ++i) {
             const int32_t o = o0 + i * TEAM + lane;
-            if (o < octs) load_oct<true>(x, o, cols_of(a.group), v[i]);
+            if (o < octs) load_oct<true, (TEAM > 4)>(x, o, cols_of(a.group), v[i]);
         }
 #pragma unroll
         for (int i = 0; i < OPL; ++i) {
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(BLOCK) k_cache_write(CacheArgs a, Split s, int
             const int32_t o = o0 + i * TEAM + lane;
             if (o < octs) {
                 const int valid = oct_valid(a.group, o);
-                if (LOOP) load_oct(x, o, cols_of(a.group), v[i]);
+                if (LOOP) load_oct<false, (TEAM > 4)>(x, o, cols_of(a.group), v[i]);
 #pragma unroll
                 for (int k = 0; k < OCT; ++k) v[i][k] = finite ? v[i][k] * inverse : 0.f;
                 store_bytes(q + o * OCT, valid, pack_oct<KIND>(v[i]));
@@ -191,7 +191,7 @@ struct CacheRead {
         const int64_t slot = g.live ? g.slot : 0;
         const int32_t grp = (int32_t)(((float)oct + 0.5f) * per_group);
         g.scale = a.scales[slot * a.scales_ld + grp];
-        load_raw((const uint8_t *)a.q + slot * a.q_ld, oct, cols_of(a.dim), g.w);
+        load_raw<false, STREAM>((const uint8_t *)a.q + slot * a.q_ld, oct, cols_of(a.dim), g.w);
     }
     template <bool STREAM>
     __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const

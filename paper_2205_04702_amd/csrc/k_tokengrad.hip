@@ -6,7 +6,7 @@
 // order in which blocks run, with fp32 sums rounded once when they are stored.  Rows
 // without a token become zeros (or stay, where the sums are added).  Three ways to
 // bring a token's positions together, by their number:
-//   up to DIRECT_MAX   every position's block looks at all tokens itself: one launch
+//   few (is_direct)    every position's block looks at all tokens itself: one launch
 //   up to RANK_MAX     every position counts the entries before its own: its place
 //   above              radix sort, stable, of (token, position)
 // After the last two, k_grad_sum walks over the sorted entries in equal pieces,
@@ -15,12 +15,24 @@
 
 namespace sp {
 
-constexpr int64_t DIRECT_MAX = 512;
+constexpr int64_t DIRECT_MAX = 1024;
+constexpr int64_t DIRECT_BLOCKS = 2048;  // positions times slabs of columns
 constexpr int64_t RANK_MAX = 8192;
 constexpr int SLAB = WAVE * OCT;  // columns of one wave
 
+// Measured on both sides of the lines (Zipf tokens, one launch or three): 1024 tokens of 128
+// columns 9 us and 14, of 1024 columns 20 and 23; 800 of 2048 columns 19 and 17.  8000
+// tokens of 128 columns, counting or sorting: 24 us and 38; 16000: 44 and 40.
+static bool is_direct(int64_t n, int64_t dim)
+{
+    return n <= DIRECT_MAX && n * ((dim + SLAB - 1) / SLAB) <= DIRECT_BLOCKS;
+}
+
 // A sorted entry: token (rows for one that is no row) above its position.
 __device__ __forceinline__ uint32_t key_of(uint64_t e) { return (uint32_t)(e >> 32); }
+
+// A value that is the same for a whole wave, held once for it.
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 template <typename IX>
 __device__ __forceinline__ uint32_t key_at(const IX *tokens, int64_t i, int64_t rows)
@@ -60,7 +72,7 @@ __device__ __forceinline__ void put_oct(const GradArgs &a, int64_t row, int32_t 
     TO *p = (TO *)a.out + row * a.out_ld;
     float w[OCT];
     if (a.add) {
-        load_oct(p, oct, cols_of(a.dim), w);
+        load_oct<false, false>(p, oct, cols_of(a.dim), w);
 #pragma unroll
         for (int k = 0; k < OCT; ++k) w[k] += a.factor * v[k];
     } else {
@@ -111,79 +123,90 @@ static int64_t fill_pieces(const GradArgs &a)
     return ((int64_t)a.dim + C - 1) / C + !aligned;
 }
 
-// Block b < sums: one position and slab of columns.  Every wave looks for the
-// position's token among all tokens, 64 at a time; the token's first position adds up
-// its rows (each wave those of every fourth group of 64 positions, joined in LDS).  The
-// other blocks write zeros to their rows without a token.
-template <typename TI, typename TO, typename IX>
-__global__ void __launch_bounds__(BLOCK) k_grad_direct(GradArgs a, int32_t slabs, int64_t sums,
-                                                       Split fill)
+// Block b < sums: one position and slab of columns.  The block's waves look for the
+// position's token among all tokens, 64 at a time, each in every eighth group of 64; at
+// the token's first position they add up its rows, wave w those of the eight places from
+// 8 w on in every group, and the first wave the waves' sums.  The other blocks write zeros to
+// their rows without a token.
+constexpr int DIRECT_NT = 512, DIRECT_WAVES = DIRECT_NT / WAVE;
+constexpr int DIRECT_GROUPS = (int)(DIRECT_MAX / WAVE);
+constexpr int DIRECT_AHEAD = 4;
+static_assert(DIRECT_MAX % DIRECT_NT == 0 && DIRECT_WAVES == 8 && DIRECT_GROUPS <= WAVE, "whole groups");
+template <typename TI, typename TO, typename IX, bool WIDE>
+__global__ void __launch_bounds__(DIRECT_NT) k_grad_direct(GradArgs a, int32_t slabs, int64_t sums,
+                                                           Split fill)
 {
-    __shared__ float part[3][SLAB];
+    __shared__ float part[DIRECT_WAVES - 1][SLAB];
+    __shared__ uint64_t found[DIRECT_GROUPS];
     __shared__ uint8_t used[FILL_UNITS];
     const IX *tokens = (const IX *)a.tokens;
     const int n = (int)a.n;
     if ((int64_t)blockIdx.x < sums) {
-        const int i = (int)(blockIdx.x / slabs);
+        const int i = (int)(blockIdx.x / slabs), w = scalar(wave_id());
         const int32_t oct = (int32_t)(blockIdx.x % slabs) * WAVE + lane_id();
         const uint32_t key = key_at(tokens, i, a.rows);
         if (key == (uint32_t)a.rows) return;
-        uint64_t mine[DIRECT_MAX / WAVE];
-        bool first = true;
+        bool earlier = false;
 #pragma unroll
-        for (int g = 0; g < (int)(DIRECT_MAX / WAVE); ++g) {
+        for (int g = w; g < DIRECT_GROUPS; g += DIRECT_WAVES) {
             const int p = g * WAVE + lane_id();
-            mine[g] = __ballot(p < n && key_at(tokens, p < n ? p : 0, a.rows) == key);
-            if (g < i / WAVE) first = first && mine[g] == 0;
-            if (g == i / WAVE) first = first && (mine[g] & ((1ull << (i % WAVE)) - 1)) == 0;
+            const bool same = p < n && key_at(tokens, p < n ? p : 0, a.rows) == key;
+            const uint64_t m = __ballot(same);
+            if (lane_id() == 0) found[g] = m;
+            earlier = earlier || (same && p < i);
         }
-        if (!first) return;  // the whole block
+        if (__syncthreads_or(earlier)) return;
         const bool on = oct * OCT < a.dim;
         float acc[OCT];
         zero_oct(acc);
+        const uint32_t places =
+            lane_id() < DIRECT_GROUPS ? (uint32_t)(found[lane_id()] >> (8 * w)) & 0xFFu : 0u;
+        uint64_t groups = __ballot(places != 0);
+        uint32_t m = 0;
+        int g = 0;
+        while (groups || m) {
+            Raw<TI> v[DIRECT_AHEAD];
+            int p[DIRECT_AHEAD];
+            bool any[DIRECT_AHEAD];
 #pragma unroll
-        for (int g = 0; g < (int)(DIRECT_MAX / WAVE); ++g) {
-            if (g % 4 != wave_id()) continue;
-            uint64_t m = mine[g];
-            while (m) {
-                Raw<TI> v[4];
-                int p[4];
-                bool any[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    any[k] = m != 0;
-                    p[k] = any[k] ? g * WAVE + __ffsll((unsigned long long)m) - 1 : i;
-                    load_raw<true>((const TI *)a.grad + p[k] * a.grad_ld, on ? oct : 0, cols_of(a.dim), v[k]);
-                    m &= m - 1;
+            for (int k = 0; k < DIRECT_AHEAD; ++k) {
+                if (!m && groups) {
+                    g = __ffsll((unsigned long long)groups) - 1;
+                    m = (uint32_t)__builtin_amdgcn_readlane((int)places, g);
+                    groups &= groups - 1;
                 }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) add_oct(a, v[k], p[k], oct, any[k], acc);
+                any[k] = m != 0;
+                p[k] = any[k] ? g * WAVE + w * 8 + __ffs(m) - 1 : i;
+                m &= m - 1;
+                load_raw<false, WIDE>((const TI *)a.grad + p[k] * a.grad_ld, on ? oct : 0, cols_of(a.dim), v[k]);
             }
-        }
-        if (wave_id() > 0) {
 #pragma unroll
-            for (int c = 0; c < OCT; ++c) part[wave_id() - 1][c * WAVE + lane_id()] = acc[c];
+            for (int k = 0; k < DIRECT_AHEAD; ++k) add_oct(a, v[k], p[k], oct, any[k], acc);
+        }
+        if (w > 0) {
+#pragma unroll
+            for (int c = 0; c < OCT; ++c) part[w - 1][c * WAVE + lane_id()] = acc[c];
         }
         __syncthreads();
-        if (wave_id() == 0 && on) {
+        if (w == 0 && on) {
 #pragma unroll
-            for (int w = 0; w < 3; ++w)
+            for (int v = 0; v < DIRECT_WAVES - 1; ++v)
 #pragma unroll
-                for (int c = 0; c < OCT; ++c) acc[c] += part[w][c * WAVE + lane_id()];
+                for (int c = 0; c < OCT; ++c) acc[c] += part[v][c * WAVE + lane_id()];
             put_oct<TO>(a, key, oct, acc);
         }
         return;
     }
     const int64_t b = (int64_t)blockIdx.x - sums;
     const int64_t row0 = b / fill.stretches * fill.rows;
-    for (int u = threadIdx.x; u < FILL_UNITS; u += BLOCK) used[u] = 0;
+    for (int u = threadIdx.x; u < FILL_UNITS; u += DIRECT_NT) used[u] = 0;
     __syncthreads();
-    for (int p = threadIdx.x; p < n; p += BLOCK) {
+    for (int p = threadIdx.x; p < n; p += DIRECT_NT) {
         const int64_t r = (int64_t)key_at(tokens, p, a.rows) - row0;
         if (r >= 0 && r < fill.rows) used[r] = 1;
     }
     __syncthreads();
-    fill_zeros<TO, BLOCK>(a, fill, b, row0, used);
+    fill_zeros<TO, DIRECT_NT>(a, fill, b, row0, used);
 }
 
 // ---------------------------------------------------------------- places by counting
@@ -391,9 +414,6 @@ __global__ void __launch_bounds__(SORT_NT) k_grad_scatter(const void *in, int64_
 constexpr int SUM_NT = 512;
 constexpr int SUM_AHEAD = 8;  // entries whose rows a team has in flight
 
-// A value that is the same for a whole wave, held once for it.
-__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
 struct SumShape {
     int32_t per;      // entries per team
     int32_t slabs;    // of LPR octets
@@ -481,7 +501,7 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
             for (int k = 0; k < SUM_AHEAD; ++k) x[k] = e[p + k < p1 ? p + k : p1 - 1];
 #pragma unroll
             for (int k = 0; k < SUM_AHEAD; ++k)
-                load_raw<true>((const TI *)a.grad + (int64_t)(uint32_t)x[k] * a.grad_ld, on ? oct : 0,
+                load_raw<true, (LPR > 4)>((const TI *)a.grad + (int64_t)(uint32_t)x[k] * a.grad_ld, on ? oct : 0,
                          cols_of(a.dim), v[k]);
 #pragma unroll
             for (int k = 0; k < SUM_AHEAD; ++k) {
@@ -584,12 +604,12 @@ __global__ void __launch_bounds__(BLOCK) k_grad_join(GradArgs a, const uint64_t 
     float acc[OCT];
     zero_oct(acc);
     if (on) {
-        if (wave_id() == 0) load_oct(part + (c * 2 + 1) * sh.part_ld, oct, whole, acc);
+        if (wave_id() == 0) load_oct<false, true>(part + (c * 2 + 1) * sh.part_ld, oct, whole, acc);
         for (int64_t j = j0; j < j1; j += 4) {
             Raw<float> v[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                load_raw(part + (j + k < j1 ? j + k : j) * 2 * sh.part_ld, oct, whole, v[k]);
+                load_raw<false, true>(part + (j + k < j1 ? j + k : j) * 2 * sh.part_ld, oct, whole, v[k]);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -641,7 +661,7 @@ struct GradWs {
 static GradWs grad_layout(int64_t n, int32_t dim)
 {
     GradWs w{};
-    if (n <= DIRECT_MAX) return w;
+    if (is_direct(n, dim)) return w;
     const auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
     w.tiles = (n + SORT_TILE - 1) / SORT_TILE;
     w.e0 = 0;
@@ -696,13 +716,13 @@ static hipError_t run_grad_as(const GradArgs &a, hipStream_t s)
 {
     const Split fill = split_rows(a.add ? 0 : a.rows, fill_pieces<TO>(a), FILL_UNITS);
     const int64_t fills = split_blocks(fill);
-    if (a.n <= DIRECT_MAX) {
+    if (is_direct(a.n, a.dim)) {
         const int32_t slabs = (int32_t)((a.dim + SLAB - 1) / SLAB);
         const int64_t sums = a.n * slabs;
         if (sums + fills == 0) return hipSuccess;
         if (sums + fills > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-        return launch(k_grad_direct<TI, TO, IX>, dim3((unsigned)(sums + fills)), dim3(BLOCK), s,
-                      a, slabs, sums, fill);
+        return launch(a.dim >= OCT ? k_grad_direct<TI, TO, IX, true> : k_grad_direct<TI, TO, IX, false>,
+                      dim3((unsigned)(sums + fills)), dim3(DIRECT_NT), s, a, slabs, sums, fill);
     }
     const GradWs w = grad_layout(a.n, a.dim);
     const SumShape sh = sum_shape(a.n, a.dim);

@@ -26,7 +26,7 @@ struct Lookup {
     __device__ __forceinline__ void load(int64_t, int32_t oct, Regs &g) const
     {
         g.live = g.t >= 0 && g.t < rows;
-        if (rows > 0) load_raw(table + (g.live ? g.t : 0) * table_ld, oct, cols_of(dim), g.r);
+        if (rows > 0) load_raw<false, STREAM>(table + (g.live ? g.t : 0) * table_ld, oct, cols_of(dim), g.r);
     }
     template <bool STREAM>
     __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const
@@ -89,8 +89,8 @@ struct Dropout {
     template <bool STREAM>
     __device__ __forceinline__ void load(int64_t row, int32_t oct, Regs &g) const
     {
-        load_raw<STREAM>(x + row * x_ld, oct, cols_of(dim), g.x);
-        if (RES) load_raw<STREAM>(residual + row * residual_ld, oct, cols_of(dim), g.r);
+        load_raw<STREAM, STREAM>(x + row * x_ld, oct, cols_of(dim), g.x);
+        if (RES) load_raw<STREAM, STREAM>(residual + row * residual_ld, oct, cols_of(dim), g.r);
     }
     template <bool STREAM>
     __device__ __forceinline__ void store(int64_t row, int32_t oct, bool fours, Regs &g) const

@@ -98,10 +98,12 @@ __device__ __forceinline__ int oct_valid(int32_t dim, int32_t oct)
     return v < OCT ? v : OCT;
 }
 
-template <bool STREAM = false, typename T>
+// WIDE: rows of 8 columns or more only.  (A branch per load, even one that all take alike,
+// keeps the loads of a thread from being issued one after the other.)
+template <bool STREAM, bool WIDE, typename T>
 __device__ __forceinline__ void load_raw(const T *row, int32_t oct, const Cols &c, Raw<T> &r)
 {
-    if (c.dim >= OCT) {
+    if (WIDE || c.dim >= OCT) {
         const int32_t col = oct * OCT, last = c.dim - OCT;
         get_bytes<STREAM, sizeof r.w>(r.w, row + (col < last ? col : last));
     } else {  // last value first, each moving the later ones up (few registers, no speed)
@@ -159,11 +161,11 @@ __device__ __forceinline__ void raw_floats(const Raw<T> &r, float (&v)[OCT])
     for (int k = 0; k < OCT; ++k) v[k] = raw_float(r, k);
 }
 
-template <bool STREAM = false, typename T>
+template <bool STREAM, bool WIDE, typename T>
 __device__ __forceinline__ void load_oct(const T *row, int32_t oct, const Cols &c, float (&v)[OCT])
 {
     Raw<T> r;
-    load_raw<STREAM>(row, oct, c, r);
+    load_raw<STREAM, WIDE>(row, oct, c, r);
     settle(r, oct, c);
     raw_floats(r, v);
 }
@@ -339,7 +341,7 @@ template <class Op>
 inline hipError_t run_octets(const Op &op, int64_t n, int64_t dim, hipStream_t st)
 {
     const int64_t width = (dim + OCT - 1) / OCT;
-    const bool deep = n * width >= OCTETS_DEEP;
+    const bool deep = n * width >= OCTETS_DEEP && dim >= OCT;
     const Split s = split_rows(n, width, deep ? 4 * BLOCK : BLOCK);
     const int64_t blocks = split_blocks(s);
     if (blocks <= 0) return hipSuccess;
