@@ -15,13 +15,13 @@
 
 namespace sp {
 
-constexpr int64_t DIRECT_MAX = 1024;
+constexpr int64_t DIRECT_MAX = 960;
 constexpr int64_t DIRECT_BLOCKS = 2048;  // positions times slabs of columns
 constexpr int64_t RANK_MAX = 8192;
 constexpr int SLAB = WAVE * OCT;  // columns of one wave
 
-// Measured on both sides of the lines (Zipf tokens, one launch or three): 1024 tokens of 128
-// columns 9 us and 14, of 1024 columns 20 and 23; 800 of 2048 columns 19 and 17.  8000
+// Measured on both sides of the lines (Zipf tokens, one launch or three): 960 tokens of 128
+// columns 9 us and 13, of 1024 columns 20 and 23; 800 of 2048 columns 19 and 17.  8000
 // tokens of 128 columns, counting or sorting: 24 us and 38; 16000: 44 and 40.
 static bool is_direct(int64_t n, int64_t dim)
 {
@@ -131,7 +131,7 @@ static int64_t fill_pieces(const GradArgs &a)
 constexpr int DIRECT_NT = 512, DIRECT_WAVES = DIRECT_NT / WAVE;
 constexpr int DIRECT_GROUPS = (int)(DIRECT_MAX / WAVE);
 constexpr int DIRECT_AHEAD = 4;
-static_assert(DIRECT_MAX % DIRECT_NT == 0 && DIRECT_WAVES == 8 && DIRECT_GROUPS <= WAVE, "whole groups");
+static_assert(DIRECT_MAX % WAVE == 0 && DIRECT_WAVES == 8 && DIRECT_GROUPS <= WAVE, "whole groups");
 template <typename TI, typename TO, typename IX, bool WIDE>
 __global__ void __launch_bounds__(DIRECT_NT) k_grad_direct(GradArgs a, int32_t slabs, int64_t sums,
                                                            Split fill)

@@ -24,6 +24,9 @@ _INDEX = {torch.int32: SP_I32, torch.int64: SP_I64}
 _KIND = {torch.int8: SP_I8, torch.float8_e4m3fn: SP_F8}
 _MASK = (1 << 64) - 1
 
+# (the public forms build objects: torch.cuda.current_stream().cuda_stream takes 1 us)
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
 _lib = None
 
 
@@ -51,12 +54,11 @@ def _bad(text):
     return sp.SPError(sp.SP_ERR_INVALID_ARG, text)
 
 
-def _type(table, t, what):
-    try:
-        return table[t.dtype if isinstance(t, torch.Tensor) else t]
-    except KeyError:
-        raise _bad(f"{what}: {getattr(t, 'dtype', t)} is none of "
-                   + ", ".join(str(k) for k in table)) from None
+def _type(table, dtype, what):
+    code = table.get(dtype)
+    if code is None:
+        raise _bad(f"{what}: {dtype} is none of " + ", ".join(str(k) for k in table))
+    return code
 
 
 def _rows(x, what, copy=True):
@@ -93,9 +95,7 @@ def _stream(stream, first, others):
     for t in others:
         if t is not None and t.get_device() != index:
             raise _bad(f"tensors on {first.device} and {t.device}")
-    if stream is None and torch._C._cuda_getDevice() == index:
-        return torch._C._cuda_getCurrentRawStream(index)
-    return None
+    return _raw_stream(index) if stream is None and _current_device() == index else None
 
 
 def _on(stream, first):
@@ -112,11 +112,14 @@ def _on(stream, first):
 
 
 def _output(out, shape, dtype, device):
+    """The output (allocated where none is given), its address and its row stride."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        out = torch.empty(shape, dtype=dtype, device=device)
+        return out, out.data_ptr(), shape[-1]
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
         raise _bad(f"out is {tuple(out.shape)} {out.dtype}, {tuple(shape)} {dtype} is needed")
-    return out
+    rows, ld = _rows(out, "out", copy=False)
+    return out, rows.data_ptr(), ld
 
 
 def _workspace(size, device, *sizes):
@@ -146,12 +149,11 @@ def lookup(tokens, table, scale=1.0, p=0.0, seed=0, offset=0, dtype=None, out=No
     rows, dim = w.shape
     if dtype is None:
         dtype = table.dtype if out is None else out.dtype
-    out = _output(out, (*tokens.shape, dim), dtype, table.device)
-    o, old = _rows(out, "out", copy=False)
+    out, to, old = _output(out, (*tokens.shape, dim), dtype, table.device)
     _check((_lib or _load()).sp_lookup(
-        ids.data_ptr(), _type(_INDEX, tokens, "tokens"), ids.shape[0], w.data_ptr(),
-        _type(_FLOAT, table, "table"), rows, dim, ld, scale, p, seed & _MASK, offset & _MASK,
-        o.data_ptr(), _type(_FLOAT, dtype, "out"), old, st))
+        ids.data_ptr(), _type(_INDEX, tokens.dtype, "tokens"), ids.shape[0], w.data_ptr(),
+        _type(_FLOAT, table.dtype, "table"), rows, dim, ld, scale, p, seed & _MASK, offset & _MASK,
+        to, _type(_FLOAT, dtype, "out"), old, st))
     return out
 
 
@@ -177,12 +179,11 @@ def lookup_grad(tokens, grad, rows, scale=1.0, p=0.0, seed=0, offset=0, dtype=No
     if dtype is None:
         dtype = torch.float32 if out is None else out.dtype
     ws = _workspace(lib.sp_lookup_grad_workspace, grad.device, n, rows, dim)
-    out = _output(out, (rows, dim), dtype, grad.device)
-    o, old = _rows(out, "out", copy=False)
+    out, to, old = _output(out, (rows, dim), dtype, grad.device)
     _check(lib.sp_lookup_grad(
-        ids.data_ptr(), _type(_INDEX, tokens, "tokens"), n, g.data_ptr(),
-        _type(_FLOAT, grad, "gradient"), dim, ld, scale, p, seed & _MASK, offset & _MASK,
-        o.data_ptr(), _type(_FLOAT, dtype, "out"), rows, old, 1 if accumulate else 0,
+        ids.data_ptr(), _type(_INDEX, tokens.dtype, "tokens"), n, g.data_ptr(),
+        _type(_FLOAT, grad.dtype, "gradient"), dim, ld, scale, p, seed & _MASK, offset & _MASK,
+        to, _type(_FLOAT, dtype, "out"), rows, old, 1 if accumulate else 0,
         *((0, 0) if ws is None else (ws.data_ptr(), ws.shape[0])), st))
     return out
 
@@ -201,13 +202,12 @@ def dropout(x, p, seed, offset=0, residual=None, out=None, stream=None):
         if residual.shape != x.shape or residual.dtype != x.dtype:
             raise _bad(f"x {tuple(x.shape)} {x.dtype}, residual {tuple(residual.shape)} {residual.dtype}")
         r, rld = _rows(residual, "residual")
-    out = _output(out, x.shape, x.dtype, x.device)
-    o, old = _rows(out, "out", copy=False)
+    out, to, old = _output(out, x.shape, x.dtype, x.device)
     n, dim = v.shape
     if dim:
         _check((_lib or _load()).sp_dropout(
-            v.data_ptr(), _type(_FLOAT, x, "x"), n, dim, ld, 0 if r is None else r.data_ptr(), rld,
-            p, seed & _MASK, offset & _MASK, o.data_ptr(), old, st))
+            v.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, ld, 0 if r is None else r.data_ptr(), rld,
+            p, seed & _MASK, offset & _MASK, to, old, st))
     return out
 
 
@@ -253,8 +253,8 @@ def cache_write(q, scales, x, slots, stream=None):
             r = x.reshape(n, dim)
     r, rld = _rows(r, "x")
     _check((_lib or _load()).sp_cache_write(
-        r.data_ptr(), _type(_FLOAT, x, "x"), n, dim, rld, at.data_ptr(),
-        _type(_INDEX, slots, "slots"), group, v.data_ptr(), _type(_KIND, q, "cache"), size, ld,
+        r.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, rld, at.data_ptr(),
+        _type(_INDEX, slots.dtype, "slots"), group, v.data_ptr(), _type(_KIND, q.dtype, "cache"), size, ld,
         s.data_ptr(), sld, st))
 
 
@@ -268,11 +268,10 @@ def cache_read(q, scales, slots, dtype=torch.bfloat16, out=None, stream=None):
     v, ld, s, sld, group = _cache(q, scales)
     at = _flat(slots)
     size, dim = v.shape
-    out = _output(out, (*slots.shape, dim), dtype, q.device)
-    o, old = _rows(out, "out", copy=False)
+    out, to, old = _output(out, (*slots.shape, dim), dtype, q.device)
     _check((_lib or _load()).sp_cache_read(
-        v.data_ptr(), _type(_KIND, q, "cache"), size, dim, ld, s.data_ptr(), sld, group,
-        at.data_ptr(), _type(_INDEX, slots, "slots"), at.shape[0], o.data_ptr(),
+        v.data_ptr(), _type(_KIND, q.dtype, "cache"), size, dim, ld, s.data_ptr(), sld, group,
+        at.data_ptr(), _type(_INDEX, slots.dtype, "slots"), at.shape[0], to,
         _type(_FLOAT, dtype, "out"), old, st))
     return out
 
@@ -294,7 +293,7 @@ def quantize(x, group=None, dtype=torch.int8, stream=None):
     q = torch.empty((n, ld), dtype=dtype, device=x.device)
     scales = torch.empty((n, dim // group), dtype=torch.float32, device=x.device)
     _check((_lib or _load()).sp_cache_write(
-        r.data_ptr(), _type(_FLOAT, x, "x"), n, dim, rld, 0, 0, group, q.data_ptr(), kind, n, ld,
+        r.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, rld, 0, 0, group, q.data_ptr(), kind, n, ld,
         scales.data_ptr(), dim // group, st))
     return (q if ld == dim else q[:, :dim]), scales
 
@@ -321,10 +320,9 @@ def product(x, x_scales, w, w_scales, dtype=torch.bfloat16, out=None, stream=Non
     b, bld = _rows(w, "w")
     xs, ws = _flat(x_scales), _flat(w_scales)
     work = _workspace(lib.sp_product_workspace, x.device, m, n, k)
-    out = _output(out, (m, n), dtype, x.device)
-    o, old = _rows(out, "out", copy=False)
+    out, to, old = _output(out, (m, n), dtype, x.device)
     _check(lib.sp_product(
-        a.data_ptr(), xs.data_ptr(), m, ald, b.data_ptr(), ws.data_ptr(), n, bld, k, o.data_ptr(),
+        a.data_ptr(), xs.data_ptr(), m, ald, b.data_ptr(), ws.data_ptr(), n, bld, k, to,
         _type(_FLOAT, dtype, "out"), old, *((0, 0) if work is None else (work.data_ptr(), work.shape[0])),
         st))
     return out
