@@ -254,9 +254,10 @@ __global__ void __launch_bounds__(RANK_NT) k_grad_rank(const IX *tokens, int32_t
 // Stable, least digit first, SORT_TILE entries per block.  Per pass the tiles count
 // their digits (hist[tile][digit]); a tile of the scatter adds up what the digits below
 // its own and the tiles before it hold, by itself while there are few tiles
-// (SELF_TILES), after k_grad_prefix otherwise.
-constexpr int SORT_NT = 512;
-constexpr int SORT_ITEMS = 8;
+// (SELF_TILES), after k_grad_prefix otherwise.  Tiles of 2048 in blocks of 16 waves: 16000
+// tokens took 40 us with 4096 in 8 waves, 32 so; 400000 took 85 and 86.
+constexpr int SORT_NT = 1024;
+constexpr int SORT_ITEMS = 2;
 constexpr int SORT_TILE = SORT_NT * SORT_ITEMS;
 constexpr int DIGIT_MAX = 9;
 constexpr int BINS_MAX = 1 << DIGIT_MAX;
