@@ -413,7 +413,10 @@ __global__ void __launch_bounds__(SORT_NT) k_grad_scatter(const void *in, int64_
 // [block][1] what begins here and continues.  Blocks after the sums write the zeros:
 // they search for their rows' entries.
 constexpr int SUM_NT = 512;
-constexpr int SUM_AHEAD = 8;  // entries whose rows a team has in flight
+// Entries whose rows a team has in flight: with a team smaller than a wave they are in vector
+// registers, and eight leave too few waves (30000 rows of 250 fp32 columns 58 us, with
+// four 47).
+constexpr int sum_ahead(int lpr) { return lpr < WAVE ? 4 : 8; }
 
 struct SumShape {
     int32_t per;      // entries per team
@@ -456,7 +459,7 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
                                                      SumShape sh, float *__restrict__ part,
                                                      Split fill)
 {
-    constexpr int TEAMS = SUM_NT / LPR;
+    constexpr int TEAMS = SUM_NT / LPR, AHEAD = sum_ahead(LPR);
     __shared__ float head[OCT][SUM_NT], tail[OCT][SUM_NT];
     __shared__ uint8_t through[TEAMS];
     __shared__ uint8_t used[FILL_UNITS];
@@ -495,17 +498,17 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
             if (is_last) through[team] = h && t;
         };
         through[team] = 0;
-        for (int64_t p = p0; p < p1; p += SUM_AHEAD) {
-            uint64_t x[SUM_AHEAD];
-            Raw<TI> v[SUM_AHEAD];
+        for (int64_t p = p0; p < p1; p += AHEAD) {
+            uint64_t x[AHEAD];
+            Raw<TI> v[AHEAD];
 #pragma unroll
-            for (int k = 0; k < SUM_AHEAD; ++k) x[k] = e[p + k < p1 ? p + k : p1 - 1];
+            for (int k = 0; k < AHEAD; ++k) x[k] = e[p + k < p1 ? p + k : p1 - 1];
 #pragma unroll
-            for (int k = 0; k < SUM_AHEAD; ++k)
+            for (int k = 0; k < AHEAD; ++k)
                 load_raw<true, (LPR > 4)>((const TI *)a.grad + (int64_t)(uint32_t)x[k] * a.grad_ld, on ? oct : 0,
                          cols_of(a.dim), v[k]);
 #pragma unroll
-            for (int k = 0; k < SUM_AHEAD; ++k) {
+            for (int k = 0; k < AHEAD; ++k) {
                 if (p + k < p1) {
                     if (key_of(x[k]) != cur) {
                         finish(false);
