@@ -406,7 +406,7 @@ sp_status sp_lookup(const void *tokens, int32_t token_type, int64_t n, const voi
  * them through, in a fixed order.  Rows without a token become zeros; with
  * accumulate != 0 the sums are added to out, and rows without a token are neither
  * read nor written.  grad [n][dim] and out [rows][dim]: SP_F32, SP_BF16 or SP_F16
- * each.  Gradients of tokens that are no rows are not read.
+ * each.  Gradients of tokens that are no rows count nothing, whatever they hold.
  * workspace: device memory of at least the bytes that sp_lookup_grad_workspace
  * gives for n, rows and dim (0 for few tokens), 16-byte aligned, in use until the
  * call's work is done; its content means nothing before and after.
@@ -443,8 +443,8 @@ sp_status sp_dropout(const void *x, int32_t type, int64_t n, int64_t dim, int64_
  * (SP_I32 or SP_I64; NULL: slot i).  scale = the group's largest magnitude / 127
  * (SP_I8) or / 448 (SP_F8), byte = x / scale rounded to nearest, ties to even.  A
  * group with an infinity or NaN reads back as NaN; one whose scale is below the
- * smallest normal fp32 number is held as zeros.  Rows whose index is no slot are not
- * read.  The slots of one call are distinct: which of two rows, or what mixture
+ * smallest normal fp32 number is held as zeros.  Rows whose index is no slot are
+ * left out.  The slots of one call are distinct: which of two rows, or what mixture
  * of them, one slot gets is not defined.
  *
  * sp_cache_read gives out[i][:] = byte * scale of slot index[i], zeros where the index
@@ -464,8 +464,9 @@ sp_status sp_cache_read(const void *q, int32_t kind, int64_t slots, int64_t dim,
  * of 8-bit integers (-128 .. 127), the sum exact (k: 1 .. 131071).  With x from
  * sp_cache_write (group = dim) the scales are those of its tokens, with w a cache
  * they are those of its rows.  out: SP_F32, SP_BF16 or SP_F16.  Fastest where x and w
- * start at, and their strides are, multiples of 16; their rows are then read in whole
- * aligned 16-byte pieces (what lies beyond k in the last one counts nothing).
+ * start at, and their strides are, multiples of 16 (and below 2^23); their rows are then
+ * read in whole aligned 16-byte pieces (what lies beyond k in the last one counts
+ * nothing).
  * workspace: as for sp_lookup_grad, of the bytes that sp_product_workspace gives for
  * m, n and k.
  */

@@ -503,6 +503,7 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
             Raw<TI> v[AHEAD];
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) x[k] = e[p + k < p1 ? p + k : p1 - 1];
+            if (key_of(x[0]) == none) break;  // nothing but padding from here on
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
                 load_raw<true, (LPR > 4)>((const TI *)a.grad + (int64_t)(uint32_t)x[k] * a.grad_ld, on ? oct : 0,
