@@ -352,6 +352,8 @@ hipError_t run_product(const ProductArgs &given, hipStream_t s)
 {
     ProductArgs a = given;
     a.stream = a.m * a.n >= 1 << 24;  // as k_octets: 32 MB of 16-bit outputs
+    if (a.m == 1) a.x_ld = 0;  // the stride of a single row aligns, and misaligns, nothing
+    if (a.n == 1) a.w_ld = 0;
     const Cut c = cut_product(a.m, a.n, a.k);
     return with_type(a.out_type, [&](auto to) {
         using TO = decltype(to);
