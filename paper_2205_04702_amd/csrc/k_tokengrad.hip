@@ -21,8 +21,9 @@ constexpr int64_t RANK_MAX = 8192;
 constexpr int SLAB = WAVE * OCT;  // columns of one wave
 
 // Measured on both sides of the lines (Zipf tokens, one launch or three): 960 tokens of 128
-// columns 9 us and 13, of 1024 columns 20 and 23; 800 of 2048 columns 19 and 17.  8000
-// tokens of 128 columns, counting or sorting: 24 us and 38; 16000: 44 and 40.
+// columns 10 us and 14, of 1024 columns 20 and 23; 800 of 2048 columns 17 either way.
+// Counting or sorting, tokens of 128 columns: 8000 counted 24 us, 9000 sorted 30; 16000
+// counted 44, sorted 32.
 static bool is_direct(int64_t n, int64_t dim)
 {
     return n <= DIRECT_MAX && n * ((dim + SLAB - 1) / SLAB) <= DIRECT_BLOCKS;
@@ -331,29 +332,45 @@ __global__ void __launch_bounds__(SORT_NT) k_grad_scatter(const void *in, int64_
 {
     constexpr int NW = SORT_NT / WAVE;
     __shared__ uint32_t cnt[NW][BINS_MAX];
+    __shared__ uint32_t sums[2][SORT_NT];
     __shared__ uint32_t lds[NW];
     const int t = (int)threadIdx.x, w = wave_id(), lane = lane_id();
     const int bins = 1 << d.bits;
     for (int b = lane; b < bins; b += WAVE) cnt[w][b] = 0;
-    // what lies before this tile's entries of digit t
+    // what lies before this tile's entries of digit t: the tiles in up to 16 parts (the chain
+    // of loads over 64 tiles was most of this kernel's time: 131072 tokens 12 us, 10 now)
     uint32_t total = 0, before = 0;
-    if (t < bins) {
-        if (prefixed) {
+    if (prefixed) {
+        if (t < bins) {
             before = hist[(int64_t)blockIdx.x << d.bits | t];
             total = hist[tiles << d.bits | t];
-        } else {
-            for (int64_t k = 0; k < tiles; k += 8) {
+        }
+    } else {
+        const int parts = SORT_NT >> d.bits < 16 ? SORT_NT >> d.bits : 16, part = t >> d.bits;
+        const int each = ((int)tiles + parts - 1) / parts, k1 = (part + 1) * each < (int)tiles ? (part + 1) * each : (int)tiles;
+        if (part < parts) {
+            const uint32_t *h = hist + (t & (bins - 1));
+            for (int k = part * each; k < k1; k += 8) {
                 uint32_t x[8];
 #pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    x[q] = k + q < tiles ? hist[(k + q) << d.bits | t] : 0u;
+                for (int q = 0; q < 8; ++q) x[q] = h[(int64_t)(k + q < k1 ? k + q : k) << d.bits];
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
+                    if (k + q >= k1) x[q] = 0;
                     total += x[q];
-                    before += k + q < (int64_t)blockIdx.x ? x[q] : 0u;
+                    before += k + q < (int)blockIdx.x ? x[q] : 0u;
                 }
             }
+            sums[0][t] = total;
+            sums[1][t] = before;
         }
+        __syncthreads();
+        total = before = 0;
+        if (t < bins)
+            for (int q = 0; q < parts; ++q) {
+                total += sums[0][q << d.bits | t];
+                before += sums[1][q << d.bits | t];
+            }
     }
     // entries, and the place of each among its wave's of the same digit: the waves
     // take consecutive stretches, the rounds of a wave follow one another
