@@ -133,7 +133,9 @@ __device__ __forceinline__ void store_bytes(uint8_t *p, int valid, uint2 w)
 // of 1024 were written at 3.9 TB/s).  The maximum is taken over the magnitudes' bits: their
 // order is that of the values, and infinity and NaN come out above everything.  A group
 // that holds one of these gets a NaN scale and zero bytes (it reads back as NaN); one
-// whose scale would be subnormal is held as zeros.
+// whose scale would be subnormal is held as zeros.  65536 rows of 1024 bf16 into random
+// slots, a scale per 128, 46 us (4.2 TB/s; 55 while the arithmetic on single values bounded it);
+// 8192 rows of 4096 with a scale each 19 us (5.2 TB/s).
 template <typename T, typename IX, int KIND, int TEAM, int OPL, int U, bool LOOP>
 __global__ void __launch_bounds__(BLOCK) k_cache_write(CacheArgs a, Split s, int32_t octs)
 {
@@ -245,7 +247,8 @@ hipError_t run_cache_write(const CacheArgs &a, hipStream_t s)
 // ---------------------------------------------------------------- read
 
 // x[i] = bytes of slot index[i] times their groups' scales; zeros where index[i]
-// is no slot.
+// is no slot.  A lookup whose rows are bytes; bound by the bytes: 65536 random rows of 1024
+// into bf16 39 us (5.2 TB/s).
 template <typename T, typename IX, int KIND>
 struct CacheRead {
     CacheArgs a;

@@ -128,7 +128,8 @@ static int64_t fill_pieces(const GradArgs &a)
 // position's token among all tokens, 64 at a time, each in every eighth group of 64; at
 // the token's first position they add up its rows, wave w those of the eight places from
 // 8 w on in every group, and the first wave the waves' sums.  The other blocks write zeros to
-// their rows without a token.
+// their rows without a token.  Bound by latency: 256 tokens of 512 columns into 8192 rows
+// (17 MB) 6 us; a token that is all of 960 costs 35 us, its rows being one block's.
 constexpr int DIRECT_NT = 512, DIRECT_WAVES = DIRECT_NT / WAVE;
 constexpr int DIRECT_GROUPS = (int)(DIRECT_MAX / WAVE);
 constexpr int DIRECT_AHEAD = 4;
@@ -215,7 +216,8 @@ __global__ void __launch_bounds__(DIRECT_NT) k_grad_direct(GradArgs a, int32_t s
 // RANK_POS positions per block; each of its 64 groups of RANK_POS lanes counts, for all of
 // them, over a 64th of the keys, four at a time from LDS.  A key before the block's own
 // positions counts where it is at most theirs, one after them where it is less; among
-// the block's own positions equal keys are counted at the end.
+// the block's own positions equal keys are counted at the end.  Bound by its compares:
+// 5003 tokens 7 us (19 with one position per lane of a whole wave, on a third of the CUs).
 constexpr int RANK_NT = 1024;
 constexpr int RANK_POS = 16;
 constexpr int RANK_PARTS = RANK_NT / RANK_POS;
@@ -428,7 +430,8 @@ __global__ void __launch_bounds__(SORT_NT) k_grad_scatter(const void *in, int64_
 // block, the first one) where the run begins adds them up in order; what crosses the
 // block's edges goes to `part`: [block][0] what continues from the block before,
 // [block][1] what begins here and continues.  Blocks after the sums write the zeros:
-// they search for their rows' entries.
+// they search for their rows' entries.  Bound by the bytes: 131072 rows of 2048 bf16 into
+// 131072 fp32 rows 303 us (1.6 GB, 5.3 TB/s), 5003 into 50001 of 1001 32 us (6.2 TB/s).
 constexpr int SUM_NT = 512;
 // Entries whose rows a team has in flight: with a team smaller than a wave they are in vector
 // registers, and eight leave too few waves (30000 rows of 250 fp32 columns 58 us, with
@@ -597,7 +600,7 @@ __global__ void __launch_bounds__(SUM_NT) k_grad_sum(GradArgs a, const uint64_t 
 }
 
 // A run that goes over the edge of chunk c and begins in it: its parts, in order.
-// Four waves take consecutive stretches of the parts.
+// Four waves take consecutive stretches of the parts.  A few dependent loads: 5 to 9 us.
 template <typename TO>
 __global__ void __launch_bounds__(BLOCK) k_grad_join(GradArgs a, const uint64_t *e, SumShape sh,
                                                      int64_t step, const float *part)

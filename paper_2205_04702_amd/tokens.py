@@ -211,11 +211,18 @@ def dropout(x, p, seed, offset=0, residual=None, out=None, stream=None):
     return out
 
 
+def _stride(dim):
+    """Bytes from row to row of 8-bit rows: product() reads whole 16-byte pieces, and 64 bytes
+    of a row at a time, which are one access where they lie in one line (55 tokens against
+    80208 rows of 3848 bytes 105 us, of 3840 bytes 78)."""
+    return (dim + 127) // 128 * 128 if dim >= 512 else (dim + 15) // 16 * 16
+
+
 def empty_cache(slots, dim, group=None, dtype=torch.int8, device="cuda"):
-    """Bytes [slots, dim] and scales [slots, dim / group] of a cache (all zeros), each row of
-    bytes starting at a multiple of 16 as product() likes it."""
+    """Bytes [slots, dim] and scales [slots, dim / group] of a cache (all zeros), the rows of
+    bytes padded as product() likes them."""
     _type(_KIND, dtype, "dtype")
-    q = torch.zeros((slots, (dim + 15) // 16 * 16), dtype=dtype, device=device)[:, :dim]
+    q = torch.zeros((slots, _stride(dim)), dtype=dtype, device=device)[:, :dim]
     return q, torch.zeros((slots, dim // (group or dim)), device=device)
 
 
@@ -289,7 +296,7 @@ def quantize(x, group=None, dtype=torch.int8, stream=None):
     kind = _type(_KIND, dtype, "dtype")
     if dim < 1 or group < 1 or dim % group:
         raise _bad(f"group {group} does not divide dim {dim}")
-    ld = (dim + 15) // 16 * 16
+    ld = _stride(dim)
     q = torch.empty((n, ld), dtype=dtype, device=x.device)
     scales = torch.empty((n, dim // group), dtype=torch.float32, device=x.device)
     _check((_lib or _load()).sp_cache_write(
@@ -301,7 +308,7 @@ def quantize(x, group=None, dtype=torch.int8, stream=None):
 def product(x, x_scales, w, w_scales, dtype=torch.bfloat16, out=None, stream=None):
     """x_scales[:, None] * w_scales * (x @ w.T) of 8-bit integer rows x [m, k] and w [n, k],
     the sums exact; one scale per row of each ([m] or [m, 1], [n] or [n, 1]).  Fastest where
-    rows start at multiples of 16 bytes, as quantize() and empty_cache() lay them out."""
+    rows start at multiples of 64 bytes, then of 16; quantize() and empty_cache() pad them so."""
     st = _stream(stream, x, (x_scales, w, w_scales, out))
     if st is None:
         with _on(stream, x):
