@@ -26,19 +26,31 @@ __device__ __forceinline__ void to_lds(const int8_t *src, int8_t *dst)
         (__attribute__((address_space(3))) void *)dst, CHUNK, 0, 0);
 }
 
-// A chunk of a row whose start or stride is no multiple of 16 bytes; bytes past the end
-// are zeros.
-__device__ __forceinline__ v4i guarded_chunk(const int8_t *row, int32_t at, int32_t k)
+// Rows whose start or stride is no multiple of 16 bytes go through registers: a chunk is
+// 16 bytes at any address.  The chunks past a row's last whole one are loaded as the
+// row's last 16 bytes and moved down by `over` bytes (16 and more: all of them).
+__device__ __forceinline__ v4i moved_down(v4i v, int over)
 {
-    v4i v = {0, 0, 0, 0};
-    if (at + CHUNK <= k) {
-        __builtin_memcpy(&v, row + at, CHUNK);
-    } else {
+    uint32_t w[4] = {(uint32_t)v.x, (uint32_t)v.y, (uint32_t)v.z, (uint32_t)v.w};
 #pragma unroll
-        for (int i = 0; i < CHUNK; ++i)
-            if (at + i < k) v[i / 4] |= (int)((uint32_t)(uint8_t)row[at + i] << (8 * (i % 4)));
+    for (int by = 4; by <= 16; by *= 2) {
+        const bool move = by == 16 ? over >= 16 : (over & by) != 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = move ? (i + by / 4 < 4 ? w[i + by / 4] : 0u) : w[i];
     }
-    return v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = __builtin_amdgcn_alignbyte(i < 3 ? w[i + 1] : 0u, w[i], over & 3);
+    return v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+}
+// The same of a row shorter than a chunk, byte by byte.
+__device__ __forceinline__ v4i short_row(const int8_t *row, int32_t at, int32_t k)
+{
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < CHUNK; ++i)
+        if (at + i < k) w[i / 4] |= (uint32_t)(uint8_t)row[at + i] << (8 * (i % 4));
+    return v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
 }
 
 // ---------------------------------------------------------------- tiles
@@ -116,20 +128,41 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
                    (uint32_t)(my_chunk * CHUNK);
     }
     const int8_t *xt = a.x + m0 * a.x_ld, *wt = a.w + n0 * a.w_ld;
-    // Load i of a step; chunks past the rows' last one take that one.
-    const auto fetch = [&](int32_t step, int i) {
+    // Load i of a step; chunks past the rows' last one take that one.  Unaligned, the load goes
+    // to registers, and the one that they held, of the step before, to LDS: three
+    // steps' loads are in LDS or on their way as well.
+    v4i held[ALIGNED ? 1 : LOADS];
+    const auto row_of = [&](int i) {
         const bool is_x = i * NW * RPL < BM;
-        int8_t *dst = sm + step % STAGES * BUF + (i * NW + wave) * RPL * KT;
-        const int32_t kb = step * KT + my_chunk * CHUNK;
+        const int64_t last = is_x ? a.m - 1 - m0 : a.n - 1 - n0;
+        const int64_t at = i * NW * RPL + my_row - (is_x ? 0 : BM);
+        return (is_x ? xt : wt) + (at < last ? at : last) * (is_x ? a.x_ld : a.w_ld);
+    };
+    const auto buffer = [&](int32_t step, int i) {
+        return sm + step % STAGES * BUF + (i * NW + wave) * RPL * KT;
+    };
+    const auto hold = [&](int32_t step, int i) {
+        const int32_t kb = step * KT + my_chunk * CHUNK, last = a.k - CHUNK;
+        __builtin_memcpy(&held[ALIGNED ? 0 : i], row_of(i) + (kb < last ? kb : last), CHUNK);
+    };
+    const auto put = [&](int32_t step, int i) {
+        v4i v = held[ALIGNED ? 0 : i];
+        if (step + 1 == all) {
+            const int32_t over = step * KT + my_chunk * CHUNK - (a.k - CHUNK);
+            v = moved_down(v, over > 0 ? over : 0);
+        }
+        *(v4i *)(buffer(step, i) + lane * CHUNK) = v;
+    };
+    const auto fetch = [&](int32_t step, int i) {
         if (ALIGNED) {
+            const bool is_x = i * NW * RPL < BM;
+            const int32_t kb = step * KT + my_chunk * CHUNK;
             const int32_t last = (a.k - 1) / CHUNK * CHUNK;
             const int32_t back = kb > last ? kb - last : 0;
-            to_lds((is_x ? xt : wt) + step * KT + (place[i] - (uint32_t)back), dst);
+            to_lds((is_x ? xt : wt) + step * KT + (place[i] - (uint32_t)back), buffer(step, i));
         } else {
-            const int64_t last = is_x ? a.m - 1 - m0 : a.n - 1 - n0;
-            const int64_t at = i * NW * RPL + my_row - (is_x ? 0 : BM);
-            const int8_t *row = (is_x ? xt : wt) + (at < last ? at : last) * (is_x ? a.x_ld : a.w_ld);
-            *(v4i *)(dst + lane * CHUNK) = guarded_chunk(row, kb, a.k);
+            put(step - 1, i);
+            hold(step, i);
         }
     };
     // Every wave's loads but its last `open` are in LDS, and every wave is done with the
@@ -181,12 +214,28 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    if (ALIGNED) {
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s)
-        if (first + s < steps) {
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (first + s < steps) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) fetch(first + s, i);
-        }
+                for (int i = 0; i < LOADS; ++i) fetch(first + s, i);
+            }
+    } else if (a.k < CHUNK) {  // one step
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            *(v4i *)(buffer(first, i) + lane * CHUNK) = short_row(row_of(i), my_chunk * CHUNK, a.k);
+    } else {  // two steps in LDS, the third held
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (first + s < steps) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) hold(first + s, i);
+                if (s < STAGES - 2) {
+#pragma unroll
+                    for (int i = 0; i < LOADS; ++i) put(first + s, i);
+                }
+            }
+    }
     landed((steps - first < STAGES - 1 ? steps - first - 1 : STAGES - 2) * LOADS);
 #pragma unroll
     for (int i = 0; i < TM + TN; ++i) read(first, 0, i);
@@ -197,6 +246,10 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
         multiply(1, s + 1, -1);
     }
     for (; s + 1 < steps; ++s) {
+        if (!ALIGNED && s + 2 < steps) {  // (once: the step still held)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) put(s + 2, i);
+        }
         multiply(0, s, -1);
         landed(s + 2 < steps ? LOADS : 0);
         multiply(1, s + 1, -1);

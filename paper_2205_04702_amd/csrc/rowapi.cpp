@@ -15,6 +15,9 @@ using namespace sp;
 
 namespace {
 
+static_assert(SP_F32 == 0 && SP_BF16 == 1 && SP_F16 == 2 && SP_I32 == 3 && SP_I64 == 4 && SP_I8 == 5 && SP_F8 == 6,
+              "the kernels' numbers of the element types");
+
 constexpr int64_t MAX_N = 0x7FFFFFFF;      // rows of one call
 constexpr int64_t MAX_DIM = 1 << 20;       // columns of a table, gradient or cache
 constexpr int64_t MAX_WIDTH = 1 << 30;     // columns of dropout's rows
