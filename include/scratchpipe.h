@@ -464,9 +464,9 @@ sp_status sp_cache_read(const void *q, int32_t kind, int64_t slots, int64_t dim,
  * of 8-bit integers (-128 .. 127), the sum exact (k: 1 .. 131071).  With x from
  * sp_cache_write (group = dim) the scales are those of its tokens, with w a cache
  * they are those of its rows.  out: SP_F32, SP_BF16 or SP_F16.  Fastest where x and w
- * start at, and their strides are, multiples of 64; slower where not of 16 (or with strides
- * of 2^23 and more), their rows going through registers.  Rows are then read in whole aligned 16-byte pieces (what
- * lies beyond k in the last one counts nothing).
+ * start at, and their strides are, multiples of 64; where they are multiples of 16 (and
+ * strides below 2^23) rows are read in whole aligned 16-byte pieces (what lies beyond k
+ * in the last one counts nothing); slower otherwise, rows going through registers.
  * workspace: as for sp_lookup_grad, of the bytes that sp_product_workspace gives for
  * m, n and k.
  */
