@@ -211,11 +211,9 @@ static hipError_t write_teams(const CacheArgs &a, hipStream_t st)
 {
     const int32_t octs = (a.group + OCT - 1) / OCT, groups = a.dim / a.group;
     const auto go = [&](auto kern, int units) {
-        const Split s = split_rows(a.n, groups, units);
-        const int64_t blocks = split_blocks(s);
-        if (blocks <= 0) return hipSuccess;
-        if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-        return launch(kern, dim3((unsigned)blocks), dim3(BLOCK), st, a, s, octs);
+        return launch_split(split_rows(a.n, groups, units), [&](const Split &s, dim3 grid) {
+            return launch(kern, grid, dim3(BLOCK), st, a, s, octs);
+        });
     };
     const auto one = [&](auto few, auto many, int team) {
         const int teams = BLOCK / team;

@@ -274,6 +274,7 @@ __device__ __forceinline__ Kept keep_oct(const Drop &d, uint32_t oct, uint32_t r
 // first row in 64.
 struct Split {
     int64_t n;        // rows
+    int64_t row0;     // the launch's first row
     int32_t width;    // units per row
     int32_t span;     // units of one row that a block takes
     int32_t rows;     // rows that a block takes (1 where span < width)
@@ -285,6 +286,7 @@ inline Split split_rows(int64_t n, int64_t width, int units)
 {
     Split s;
     s.n = n;
+    s.row0 = 0;
     s.width = (int32_t)width;
     s.span = (int32_t)(width < units ? width : units);
     s.rows = units / s.span;
@@ -294,6 +296,22 @@ inline Split split_rows(int64_t n, int64_t width, int units)
     return s;
 }
 inline int64_t split_blocks(const Split &s) { return (s.n + s.rows - 1) / s.rows * s.stretches; }
+
+// A launch has fewer than 2^32 threads along an axis.  go(split, blocks) launches one piece of
+// a split, whole rows of blocks, of at most 2^23 blocks (of up to 511 threads).
+constexpr int64_t LAUNCH_BLOCKS = 1 << 23;
+template <class F>
+inline hipError_t launch_split(Split s, F go)
+{
+    const int64_t row_blocks = (s.n + s.rows - 1) / s.rows, each = LAUNCH_BLOCKS / s.stretches;
+    for (int64_t b = 0; b < row_blocks; b += each) {
+        const int64_t k = row_blocks - b < each ? row_blocks - b : each;
+        s.row0 = b * s.rows;
+        const hipError_t e = go(s, dim3((unsigned)(k * s.stretches)));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 // Unit u of block b: its row and its place in the row; false where there is none.
 __device__ __forceinline__ bool split_at(const Split &s, int64_t b, int u, int64_t &row,
@@ -307,7 +325,7 @@ __device__ __forceinline__ bool split_at(const Split &s, int64_t b, int u, int64
     }
     const int r = (int)(((float)u + 0.5f) * s.inv);
     at = st * s.span + (u - r * s.span);
-    row = rb * s.rows + r;
+    row = s.row0 + rb * s.rows + r;
     return r < s.rows && row < s.n && at < s.width;
 }
 
@@ -342,12 +360,10 @@ inline hipError_t run_octets(const Op &op, int64_t n, int64_t dim, hipStream_t s
 {
     const int64_t width = (dim + OCT - 1) / OCT;
     const bool deep = n * width >= OCTETS_DEEP && dim >= OCT;
-    const Split s = split_rows(n, width, deep ? 4 * BLOCK : BLOCK);
-    const int64_t blocks = split_blocks(s);
-    if (blocks <= 0) return hipSuccess;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    return deep ? launch(k_octets<Op, 4>, dim3((unsigned)blocks), dim3(BLOCK), st, op, s)
-                : launch(k_octets<Op, 1>, dim3((unsigned)blocks), dim3(BLOCK), st, op, s);
+    return launch_split(split_rows(n, width, deep ? 4 * BLOCK : BLOCK), [&](const Split &s, dim3 grid) {
+        return deep ? launch(k_octets<Op, 4>, grid, dim3(BLOCK), st, op, s)
+                    : launch(k_octets<Op, 1>, grid, dim3(BLOCK), st, op, s);
+    });
 }
 
 // ---------------------------------------------------------------- element types
