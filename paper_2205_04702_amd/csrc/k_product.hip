@@ -17,7 +17,6 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 constexpr int KT = 64;      // bytes of a row in one step
 constexpr int STAGES = 4;   // steps that LDS holds
 constexpr int CHUNK = 16;   // bytes of one access
-constexpr int LONG_K = 4096;
 
 __device__ __forceinline__ void to_lds(const int8_t *src, int8_t *dst)
 {
@@ -79,20 +78,18 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
     constexpr int BUF = (BM + BN) * KT;
     __shared__ __attribute__((aligned(16))) int8_t sm[STAGES * BUF];
     const int wave = wave_id(), lane = lane_id();
-    // Which tile.  Short rows: each XCD takes a stretch of the tiles, in groups of four columns
-    // of tiles, so that what runs on it at a time (8 x 4 tiles, say, of 12 tiles' rows) shares
-    // its L2 and rows of w are read by one XCD.  Long rows: tile after tile along a row of
-    // tiles, XCD after XCD.  (3000 x 20000 x 300 47 us and 55, 8000 x 1000 x 2000 28 and 29;
-    // 8192 x 16384 x 4096 from memory 545 and 537.)
-    uint32_t tile_m = blockIdx.x / (uint32_t)tiles_n, tile_n = blockIdx.x - tile_m * (uint32_t)tiles_n;
-    if (a.k < LONG_K) {
-        const uint32_t tiles_m = gridDim.x / (uint32_t)tiles_n;
-        const uint32_t tile = (uint32_t)xcd_block(blockIdx.x, gridDim.x);
-        const uint32_t group = tile / (4u * tiles_m), in = tile - group * 4u * tiles_m;
-        const uint32_t wide = (uint32_t)tiles_n - group * 4u < 4u ? (uint32_t)tiles_n - group * 4u : 4u;
-        tile_m = in / wide;
-        tile_n = group * 4u + in % wide;
-    }
+    // Which tile: each XCD takes a stretch of the tiles, in groups of four columns of tiles, so
+    // that what runs on it at a time (8 x 4 tiles, say, of 12 tiles' rows) shares its L2 and
+    // rows of w are read by one XCD.  Against tile after tile along a row of tiles, XCD after
+    // XCD (us, rows past the caches): 16384 x 2048 x 8192 250 and 274, x 2048 77 and 83,
+    // 1000 x 60000 x 4096 262 and 280, 5000 x 5000 x 5000 139 and 145, 3000 x 20000 x 2000 139 and
+    // 147; with 64 columns of tiles the other way round, 8192 x 16384 x 512 128 and 122, x 4096
+    // 512 and 507; in 23 more shapes, k from 300 to 8192, up to 7 % less or 4 % more.
+    const uint32_t tiles_m = gridDim.x / (uint32_t)tiles_n;
+    const uint32_t tile = (uint32_t)xcd_block(blockIdx.x, gridDim.x);
+    const uint32_t group = tile / (4u * tiles_m), in = tile - group * 4u * tiles_m;
+    const uint32_t wide = (uint32_t)tiles_n - group * 4u < 4u ? (uint32_t)tiles_n - group * 4u : 4u;
+    const uint32_t tile_m = in / wide, tile_n = group * 4u + in % wide;
     const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
     constexpr bool PARTIAL = std::is_same<TO, int32_t>::value;  // sums of a part of k
     const int32_t first = (int32_t)blockIdx.y * per_split;
