@@ -302,8 +302,7 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
             TO *p = out + (int64_t)(i * 32 + r0) * a.out_ld;
             if (m0 + wm + i * 32 + r0 + lane / LPR >= a.m) continue;
             if (n + EP <= a.n) {
-                if (a.stream) put_bytes<true, sizeof o>(p, &o);
-                else put_bytes<false, sizeof o>(p, &o);
+                put_bytes<false, sizeof o>(p, &o);
             } else {
 #pragma unroll
                 for (int c = 0; c < EP; ++c)
@@ -419,7 +418,6 @@ static hipError_t run_cut(const ProductArgs &a, const Cut &c, hipStream_t s)
 hipError_t run_product(const ProductArgs &given, hipStream_t s)
 {
     ProductArgs a = given;
-    a.stream = a.m * a.n >= 1 << 24;  // as k_octets: 32 MB of 16-bit outputs
     if (a.m == 1) a.x_ld = 0;  // the stride of a single row aligns, and misaligns, nothing
     if (a.n == 1) a.w_ld = 0;
     const Cut c = cut_product(a.m, a.n, a.k);
@@ -428,7 +426,6 @@ hipError_t run_product(const ProductArgs &given, hipStream_t s)
         if (c.splits == 1) return run_cut<TO>(a, c, s);
         ProductArgs p = a;
         p.out_ld = a.n;
-        p.stream = false;
         hipError_t r = run_cut<int32_t>(p, c, s);
         if (r != hipSuccess) return r;
         const int32_t steps = (a.k + KT - 1) / KT, per = (steps + c.splits - 1) / c.splits;

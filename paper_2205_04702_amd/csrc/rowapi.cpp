@@ -233,6 +233,6 @@ extern "C" sp_status sp_product(const int8_t *x, const float *x_scales, int64_t 
                    (long long)need);
     if (need > 0 && (uintptr_t)workspace % 16 != 0) return bad("workspace is not aligned to 16 bytes");
     const ProductArgs a{x, w, x_scales, w_scales, m, n, (int32_t)k, x_ld, w_ld, out, out_type, out_ld,
-                        (char *)workspace, false};
+                        (char *)workspace};
     return done(run_product(a, (hipStream_t)stream), "sp_product");
 }

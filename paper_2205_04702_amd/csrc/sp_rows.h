@@ -461,7 +461,6 @@ struct ProductArgs {
     int32_t out_type;
     int64_t out_ld;
     char *work;
-    bool stream;  // outputs past the caches
 };
 int64_t product_workspace(int64_t m, int64_t n, int64_t k);
 hipError_t run_product(const ProductArgs &a, hipStream_t s);
