@@ -68,7 +68,7 @@ __device__ __forceinline__ v4i short_row(const int8_t *row, int32_t at, int32_t 
 // the counters; matrix instructions alone took 368 us), the matrix cores busy two thirds
 // of the time.  What a CU loads bounds smaller tiles: 12 to 13 TB/s from L2 together.
 template <int BM, int BN, int WM, int WN, typename TO, bool ALIGNED>
-__global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs a, int32_t tiles_n, int32_t per_split)
+__global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs a, int32_t tiles_n, uint32_t tiles_m, int32_t per_split)
 {
     constexpr int NW = (BM / WM) * (BN / WN), NT = NW * WAVE;
     constexpr int TM = WM / 32, TN = WN / 32;
@@ -84,12 +84,17 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
     // XCD (us, rows past the caches): 16384 x 2048 x 8192 250 and 274, x 2048 77 and 83,
     // 1000 x 60000 x 4096 262 and 280, 5000 x 5000 x 5000 139 and 145, 3000 x 20000 x 2000 139 and
     // 147; with 64 columns of tiles the other way round, 8192 x 16384 x 512 128 and 122, x 4096
-    // 512 and 507; in 23 more shapes, k from 300 to 8192, up to 7 % less or 4 % more.
-    const uint32_t tiles_m = gridDim.x / (uint32_t)tiles_n;
-    const uint32_t tile = (uint32_t)xcd_block(blockIdx.x, gridDim.x);
-    const uint32_t group = tile / (4u * tiles_m), in = tile - group * 4u * tiles_m;
-    const uint32_t wide = (uint32_t)tiles_n - group * 4u < 4u ? (uint32_t)tiles_n - group * 4u : 4u;
-    const uint32_t tile_m = in / wide, tile_n = group * 4u + in % wide;
+    // 512 and 507; in 23 more shapes, k from 300 to 8192, up to 7 % less or 4 % more.  One row of
+    // tiles has nothing to share, and the divisions' time to lose: 64 x 4096 x 4096 13.3 in
+    // groups, 12.5 without.
+    uint32_t tile_m = 0, tile_n = blockIdx.x;
+    if (tiles_m > 1) {
+        const uint32_t tile = (uint32_t)xcd_block(blockIdx.x, gridDim.x);
+        const uint32_t group = tile / (4u * tiles_m), in = tile - group * 4u * tiles_m;
+        const uint32_t wide = (uint32_t)tiles_n - group * 4u < 4u ? (uint32_t)tiles_n - group * 4u : 4u;
+        tile_m = in / wide;
+        tile_n = group * 4u + in % wide;
+    }
     const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
     constexpr bool PARTIAL = std::is_same<TO, int32_t>::value;  // sums of a part of k
     const int32_t first = (int32_t)blockIdx.y * per_split;
@@ -401,8 +406,8 @@ static hipError_t run_tiles(const ProductArgs &a, int32_t splits, hipStream_t s)
     if (tm * tn > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
     const int32_t steps = (a.k + KT - 1) / KT, per = (steps + splits - 1) / splits;
     const dim3 grid((unsigned)(tm * tn), (unsigned)((steps + per - 1) / per)), block(BM / WM * (BN / WN) * WAVE);
-    return aligned ? launch(k_product<BM, BN, WM, WN, TO, true>, grid, block, s, a, (int32_t)tn, per)
-                   : launch(k_product<BM, BN, WM, WN, TO, false>, grid, block, s, a, (int32_t)tn, per);
+    return aligned ? launch(k_product<BM, BN, WM, WN, TO, true>, grid, block, s, a, (int32_t)tn, (uint32_t)tm, per)
+                   : launch(k_product<BM, BN, WM, WN, TO, false>, grid, block, s, a, (int32_t)tn, (uint32_t)tm, per);
 }
 
 template <typename TO>
