@@ -256,20 +256,25 @@ __global__ void __launch_bounds__(RANK_NT) k_grad_rank(const IX *tokens, int32_t
 
 // Stable, least digit first, SORT_TILE entries per block.  Per pass the tiles count
 // their digits (hist[tile][digit]); a tile of the scatter adds up what the digits below
-// its own and the tiles before it hold, by itself while there are few tiles
-// (SELF_TILES), after k_grad_prefix otherwise.  Tiles of 2048 in blocks of 16 waves: 16000
+// its own and the tiles before it hold, by itself while there are few tiles, after
+// k_grad_prefix otherwise.  Its threads share the tiles in `parts`, as many as its threads
+// hold digits (2 of nine bits, 16 of five), and the line lies where a part has SELF_TILES.
+// By itself and after the prefix (whole gradients of 16 columns, us): two parts, 196 tiles 75
+// and 81, 293 116 and 102; four, 489 99 and 110, 733 167 and 164; eight, 733 206 and 251, 1465
+// 465 and 449; sixteen, 1465 193 and 274.  Tiles of 2048 in blocks of 16 waves: 16000
 // tokens took 40 us with 4096 in 8 waves, 32 so; 400000 took 85 and 86.
 constexpr int SORT_NT = 1024;
 constexpr int SORT_ITEMS = 2;
 constexpr int SORT_TILE = SORT_NT * SORT_ITEMS;
 constexpr int DIGIT_MAX = 9;
 constexpr int BINS_MAX = 1 << DIGIT_MAX;
-constexpr int SELF_TILES = 64;
+constexpr int SELF_TILES = 128;
 static_assert(BINS_MAX <= SORT_NT, "one thread per digit");
 
 struct Digits {
     int32_t shift, bits;
 };
+__host__ __device__ constexpr int sort_parts(int bits) { return SORT_NT >> bits < 16 ? SORT_NT >> bits : 16; }
 
 template <typename IX, bool FIRST>
 __device__ __forceinline__ uint64_t sort_entry(const void *in, int64_t i, int64_t rows)
@@ -340,7 +345,7 @@ __global__ void __launch_bounds__(SORT_NT) k_grad_scatter(const void *in, int64_
     const int bins = 1 << d.bits;
     for (int b = lane; b < bins; b += WAVE) cnt[w][b] = 0;
     // what lies before this tile's entries of digit t: the tiles in up to 16 parts (the chain
-    // of loads over 64 tiles was most of this kernel's time: 131072 tokens 12 us, 10 now)
+    // of loads over 64 tiles was most of this kernel's time: 131072 tokens 12 us, 10 so)
     uint32_t total = 0, before = 0;
     if (prefixed) {
         if (t < bins) {
@@ -348,7 +353,7 @@ __global__ void __launch_bounds__(SORT_NT) k_grad_scatter(const void *in, int64_
             total = hist[tiles << d.bits | t];
         }
     } else {
-        const int parts = SORT_NT >> d.bits < 16 ? SORT_NT >> d.bits : 16, part = t >> d.bits;
+        const int parts = sort_parts(d.bits), part = t >> d.bits;
         const int each = ((int)tiles + parts - 1) / parts, k1 = (part + 1) * each < (int)tiles ? (part + 1) * each : (int)tiles;
         if (part < parts) {
             const uint32_t *h = hist + (t & (bins - 1));
@@ -714,7 +719,7 @@ static hipError_t sort_tokens(const GradArgs &a, const GradWs &w, uint64_t **sor
     const int passes = (bits + DIGIT_MAX - 1) / DIGIT_MAX, width = (bits + passes - 1) / passes;
     uint32_t *hist = (uint32_t *)(a.ws + w.hist);
     const dim3 grid((unsigned)w.tiles), block(SORT_NT);
-    const bool prefixed = w.tiles > SELF_TILES;
+    const bool prefixed = w.tiles > (int64_t)SELF_TILES * sort_parts(width);
     const void *in = a.tokens;
     uint64_t *out = e0;
     for (int p = 0; p < passes; ++p) {
