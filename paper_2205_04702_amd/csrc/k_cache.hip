@@ -249,6 +249,8 @@ hipError_t run_cache_write(const CacheArgs &a, hipStream_t s)
 // into bf16 39 us (5.2 TB/s).
 template <typename T, typename IX, int KIND>
 struct CacheRead {
+    static constexpr bool DEEP = true;
+    bool deep_pays() const { return whole_pieces((const T *)a.x, a.x_ld); }
     CacheArgs a;
     float per_group;  // octets of a group, inverted; 0: one group
     struct Regs {

@@ -12,6 +12,8 @@ namespace sp {
 // 2048 without 245 us, 4.4 TB/s).  Outputs go past the caches there, the table does not: tokens repeat.
 template <typename TI, typename TO, typename IX, bool DROP>
 struct Lookup {
+    static constexpr bool DEEP = true;
+    bool deep_pays() const { return whole_pieces(out, out_ld); }
     const IX *tokens;
     const TI *table;
     TO *out;
@@ -78,9 +80,12 @@ hipError_t run_lookup(const LookupArgs &a, hipStream_t s)
 // out = [residual +] factor * keep * x.  The backward pass is the same call on
 // the gradient: the mask is drawn again from seed, offset and place.  Bound by the bytes,
 // each moved once: 16384 x 4096 in bf16 with a residual 65 us, 6.2 TB/s past the caches
-// (78 us through them).
+// (78 us through them).  fp32 takes an octet per thread, near the caches, at any size: 8192 x 4096 49
+// us, 54 deep; of 250 columns, 2^22 octets, 54 and 70.
 template <typename T, bool RES>
 struct Dropout {
+    static constexpr bool DEEP = sizeof(T) < 4;
+    bool deep_pays() const { return true; }
     const T *x, *residual;
     T *out;
     int64_t x_ld, residual_ld, out_ld;

@@ -352,18 +352,36 @@ __global__ void __launch_bounds__(BLOCK) k_octets(Op op, Split s)
 }
 
 // Four octets per thread, outputs (and inputs that are read once) past the caches, where
-// there are octets for that: 32 MB of 16-bit values, what the L2s hold together.  Below, one
-// octet per thread, and the outputs stay near for the next kernel.
-constexpr int64_t OCTETS_DEEP = 1 << 21;
+// there are octets for that and the operator allows it (DEEP) and says that it pays.  Below,
+// one octet per thread, and the outputs stay near for the next kernel.  Deep and not (us,
+// inputs past the caches, rows of 1024 bf16 columns): 2^19 octets lookup 4.4 and 5.5, dropout
+// with a residual 6.9 and 6.8, cache read 4.6 and 4.8; 2^20 6.8 and 9.5, 11.5 and 12.0, 6.3 and
+// 8.6; 2^22 21.8 and 27.0, 35.2 and 37.0, 15.6 and 23.5.  A lookup and two dropouts of what it
+// gave, one after the other: 2^19 15.0 and 14.7, 2^20 22.0 and 23.1, 2^22 72 and 70.
+constexpr int64_t OCTETS_DEEP = 1 << 20;
 template <class Op>
 inline hipError_t run_octets(const Op &op, int64_t n, int64_t dim, hipStream_t st)
 {
     const int64_t width = (dim + OCT - 1) / OCT;
-    const bool deep = n * width >= OCTETS_DEEP && dim >= OCT;
-    return launch_split(split_rows(n, width, deep ? 4 * BLOCK : BLOCK), [&](const Split &s, dim3 grid) {
-        return deep ? launch(k_octets<Op, 4>, grid, dim3(BLOCK), st, op, s)
-                    : launch(k_octets<Op, 1>, grid, dim3(BLOCK), st, op, s);
+    if constexpr (Op::DEEP) {
+        if (n * width >= OCTETS_DEEP && dim >= OCT && op.deep_pays())
+            return launch_split(split_rows(n, width, 4 * BLOCK), [&](const Split &s, dim3 grid) {
+                return launch(k_octets<Op, 4>, grid, dim3(BLOCK), st, op, s);
+            });
+    }
+    return launch_split(split_rows(n, width, BLOCK), [&](const Split &s, dim3 grid) {
+        return launch(k_octets<Op, 1>, grid, dim3(BLOCK), st, op, s);
     });
+}
+
+// For rows that are looked up deep pays but where they are fp32 and share 32-byte pieces, which
+// past the caches are written in parts (us, deep and not, 2^22 octets: cached rows read into
+// fp32 of 250 columns 55 and 41, 1001 60 and 47, 2048 34 and 40, 24 32 and 49; bf16 rows looked
+// up into the same 55 and 43, 53 and 52, 44 and 41, 38 and 47).
+template <typename TO>
+inline bool whole_pieces(const TO *out, int64_t ld)
+{
+    return sizeof(TO) < 4 || ((uintptr_t)out | (uint64_t)ld * sizeof(TO)) % 32 == 0;
 }
 
 // ---------------------------------------------------------------- element types

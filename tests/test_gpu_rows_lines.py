@@ -111,3 +111,43 @@ def test_several_threads():
         t.join()
     for i in range(4):
         assert len(together[i]) == 4 and all(torch.equal(a, b) for a, b in zip(alone[i], together[i]))
+
+
+@pytest.mark.parametrize("n,dim,ld,left", [(130_000, 65, 72, 0), (130_000, 65, 72, 8), (130_000, 65, 72, 1),
+                                           (130_000, 65, 67, 0), (40_000, 256, 256, 0), (40_000, 250, 250, 0)])
+@pytest.mark.parametrize("out", [F32, BF16])
+def test_many_rows_into_whole_and_shared_pieces(n, dim, ld, left, out):
+    """More than 2^20 octets, fp32 rows at multiples of 32 bytes and elsewhere: a lookup and a read of
+    the cache give what a few rows at a time give, and keep to their columns."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + dim)
+    w = torch.randn((500, dim), generator=g, device="cuda")
+    tok = torch.randint(-20, 520, (n,), generator=g, device="cuda")
+    q, s = tk.quantize(w)
+    for call in (lambda t, o: tk.lookup(t, w, 1.5, out=o), lambda t, o: tk.cache_read(q, s, t, dtype=out, out=o)):
+        buf = torch.full((n, left + ld), 9.0, dtype=out, device="cuda")
+        call(tok, buf[:, left:left + dim])
+        few = torch.empty((1000, dim), dtype=out, device="cuda")
+        every = torch.cat([torch.arange(500, device="cuda"), torch.full((500,), -1, device="cuda")])
+        call(every, few)
+        where = torch.where((tok >= 0) & (tok < 500), tok, torch.full_like(tok, 999))
+        assert torch.equal(buf[:, left:left + dim], few[where])
+        assert (buf[:, :left] == 9).all() and (buf[:, left + dim:] == 9).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("octets", [2 ** 20 - 1000, 2 ** 20, 2 ** 21])
+def test_dropout_around_its_deep_form(dtype, octets):
+    dim = 1000
+    n = octets // 125 + 1
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x, r = torch.randn((n, dim), generator=g, device="cuda").to(dtype), torch.randn((n, dim), device="cuda").to(dtype)
+    got = tk.dropout(x, 0.25, 8, 9, residual=r)
+    assert torch.equal(got[:700], tk.dropout(x[:700], 0.25, 8, 9, residual=r[:700]))
+    mask = tk.dropout(torch.ones((n, dim), device="cuda"), 0.25, 8, 9) != 0
+    assert torch.equal(mask[:50].cpu(), ref.keep_mask(50, dim, 0.25, 8, 9))
+    y = torch.where(mask, x.double() / 0.75, torch.zeros((), dtype=torch.float64, device="cuda"))
+    want = y + r.double()
+    off = (got.double() - want).abs() - (y.abs() * 3 * U32 + want.abs() * (ref.UNIT[dtype] + 2 * U32) + ref.TINY[dtype])
+    assert off.max().item() <= 0
