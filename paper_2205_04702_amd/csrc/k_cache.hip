@@ -205,7 +205,10 @@ __global__ void __launch_bounds__(BLOCK) k_cache_write(CacheArgs a, Split s, int
     }
 }
 
-// Four groups per team where that leaves blocks enough for the card, one otherwise.
+// Four groups per team where that leaves blocks enough for the card, one otherwise: with 512
+// blocks of four 6.6 us and 5.5 with one each (4096 rows of 1024 bf16, a scale per 128, random
+// slots), with 1024 9.0 either way, 2048 13.5 and 15.1, 16384 78 and 93; groups of 64, 256 and 512
+// the same within 3 %.
 template <typename T, typename IX, int KIND>
 static hipError_t write_teams(const CacheArgs &a, hipStream_t st)
 {

@@ -671,7 +671,10 @@ static int team_lanes(int32_t dim)
 
 // Pieces of 4 to 32 entries per team: enough blocks for the card where there are few
 // entries, few cut runs where there are many.  Narrow rows have many teams in a block and
-// take 8 or 16 at least: a run goes from team to team in turn.
+// take 8 or 16 at least: a run goes from team to team in turn.  Whole gradients, us, with 256,
+// 512, 1024, 2048 and 4096 blocks aimed at: 131072 x 512 107 107 104 104 121, 1000000 x 256 239 239
+// 239 246 251, 20000 x 2048 98 91 91 93 93, narrow or few rows the same within 2 %; with 8, 16, 32,
+// 64 and 128 entries at most: 131072 x 2048 355 346 339 342 343, 1000000 x 256 266 246 239 256 256.
 static SumShape sum_shape(int64_t n, int32_t dim)
 {
     const int lpr = team_lanes(dim), teams = SUM_NT / lpr;
