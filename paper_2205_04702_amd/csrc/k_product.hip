@@ -403,7 +403,24 @@ static hipError_t run_tiles(const ProductArgs &a, int32_t splits, hipStream_t s)
         ((uintptr_t)a.x | (uintptr_t)a.w | (uint64_t)a.x_ld | (uint64_t)a.w_ld) % CHUNK == 0 &&
         a.x_ld < 1 << 23 && a.w_ld < 1 << 23;
     const int64_t tm = (a.m + BM - 1) / BM, tn = (a.n + BN - 1) / BN;
-    if (tm * tn > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    if (tm * tn > LAUNCH_BLOCKS / 2) {  // (up to 512 threads each; never in parts of k)
+        ProductArgs lo = a, hi = a;
+        if (tm >= tn) {
+            lo.m = tm / 2 * BM;
+            hi.m = a.m - lo.m;
+            hi.x += lo.m * a.x_ld;
+            hi.xs += lo.m;
+            hi.out = (TO *)a.out + lo.m * a.out_ld;
+        } else {
+            lo.n = tn / 2 * BN;
+            hi.n = a.n - lo.n;
+            hi.w += lo.n * a.w_ld;
+            hi.ws += lo.n;
+            hi.out = (TO *)a.out + lo.n;
+        }
+        const hipError_t r = run_tiles<BM, BN, WM, WN, TO>(lo, splits, s);
+        return r != hipSuccess ? r : run_tiles<BM, BN, WM, WN, TO>(hi, splits, s);
+    }
     const int32_t steps = (a.k + KT - 1) / KT, per = (steps + splits - 1) / splits;
     const dim3 grid((unsigned)(tm * tn), (unsigned)((steps + per - 1) / per)), block(BM / WM * (BN / WN) * WAVE);
     return aligned ? launch(k_product<BM, BN, WM, WN, TO, true>, grid, block, s, a, (int32_t)tn, (uint32_t)tm, per)

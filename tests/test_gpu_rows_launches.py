@@ -60,3 +60,22 @@ def test_lookup_of_more_rows_than_a_launch_has():
             keep = torch.tensor([words[e // 2] >> (16 * (e % 2)) & 0xFFFF for e in range(8)]) >= drop
             live = w[3, octet * 8:octet * 8 + 8] != 0
             assert torch.equal((got[row, octet * 8:octet * 8 + 8] != 0).cpu(), keep & live.cpu())
+
+
+def test_product_of_more_tiles_than_a_launch_has():
+    """2^30 rows and more on either side: 2^24 tiles of 64 rows."""
+    room(70)
+    n, k = 2 ** 30 + 130, 16
+    x = torch.empty((n, k), dtype=torch.int8, device="cuda")
+    for i in range(0, n, 2 ** 26):
+        x[i:i + 2 ** 26].random_(-128, 128)
+    xs = torch.rand(n, device="cuda")
+    y, ys = x[-3:].clone(), torch.rand(3, device="cuda")
+    step = 2 ** 24
+    got = tk.product(x, xs, y, ys)
+    for i in range(0, n, step):
+        assert torch.equal(got[i:i + step], tk.product(x[i:i + step], xs[i:i + step], y, ys))
+    got = None
+    got = tk.product(y, ys, x, xs)
+    for i in range(0, n, step):
+        assert torch.equal(got[:, i:i + step], tk.product(y, ys, x[i:i + step], xs[i:i + step]))
