@@ -218,12 +218,21 @@ def _stride(dim):
     return (dim + 127) // 128 * 128 if dim >= 512 else (dim + 15) // 16 * 16
 
 
+def _groups(dim, group):
+    """The scales of a row."""
+    group = group or dim
+    if dim < 1 or group < 1 or dim % group:
+        raise _bad(f"group {group} does not divide dim {dim}")
+    return dim // group
+
+
 def empty_cache(slots, dim, group=None, dtype=torch.int8, device="cuda"):
     """Bytes [slots, dim] and scales [slots, dim / group] of a cache (all zeros), the rows of
     bytes padded as product() likes them."""
     _type(_KIND, dtype, "dtype")
+    groups = _groups(dim, group)
     q = torch.zeros((slots, _stride(dim)), dtype=dtype, device=device)[:, :dim]
-    return q, torch.zeros((slots, dim // (group or dim)), device=device)
+    return q, torch.zeros((slots, groups), device=device)
 
 
 def _cache(q, scales):
@@ -292,16 +301,14 @@ def quantize(x, group=None, dtype=torch.int8, stream=None):
             return quantize(x, group, dtype)
     r, rld = _rows(x, "x")
     n, dim = r.shape
-    group = group or dim
+    groups = _groups(dim, group)
     kind = _type(_KIND, dtype, "dtype")
-    if dim < 1 or group < 1 or dim % group:
-        raise _bad(f"group {group} does not divide dim {dim}")
     ld = _stride(dim)
     q = torch.empty((n, ld), dtype=dtype, device=x.device)
-    scales = torch.empty((n, dim // group), dtype=torch.float32, device=x.device)
+    scales = torch.empty((n, groups), dtype=torch.float32, device=x.device)
     _check((_lib or _load()).sp_cache_write(
-        r.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, rld, 0, 0, group, q.data_ptr(), kind, n, ld,
-        scales.data_ptr(), dim // group, st))
+        r.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, rld, 0, 0, dim // groups, q.data_ptr(), kind, n, ld,
+        scales.data_ptr(), groups, st))
     return (q if ld == dim else q[:, :dim]), scales
 
 
