@@ -9,12 +9,19 @@ of the HIP library on the current stream (or the one given), torch tensors out.
     q, scales = quantize(table)                                 # serving: rows in 8 bits
     cache_write(q, scales, x, slots); x = cache_read(q, scales, slots)
     scores = product(*quantize(x), q, scales)
+
+Autograd does not see these calls: what they return requires no gradient even where an input
+does, and gradients are taken by calls of their own (lookup_grad; dropout on the gradient).
+What a call writes into (out, a cache) counts as changed in place, so a graph that saved it
+refuses to go backward over it.  A call on a given stream waits for no other: what it reads
+has to be ready there, and to stay allocated until it is done.
 """
 from __future__ import annotations
 
 import ctypes as C
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import scratchpipe as sp
 
@@ -133,6 +140,12 @@ def _check(status):
         sp._check(status)
 
 
+def _changed(given):
+    """What the caller handed in to be written into (or None), for autograd's checks."""
+    if given is not None:
+        increment_version(given)
+
+
 def lookup(tokens, table, scale=1.0, p=0.0, seed=0, offset=0, dtype=None, out=None, stream=None):
     """scale * table[tokens], [*tokens.shape, dim], with dropout of probability p.
 
@@ -149,12 +162,13 @@ def lookup(tokens, table, scale=1.0, p=0.0, seed=0, offset=0, dtype=None, out=No
     rows, dim = w.shape
     if dtype is None:
         dtype = table.dtype if out is None else out.dtype
-    out, to, old = _output(out, (*tokens.shape, dim), dtype, table.device)
+    looked_up, to, old = _output(out, (*tokens.shape, dim), dtype, table.device)
     _check((_lib or _load()).sp_lookup(
         ids.data_ptr(), _type(_INDEX, tokens.dtype, "tokens"), ids.shape[0], w.data_ptr(),
         _type(_FLOAT, table.dtype, "table"), rows, dim, ld, scale, p, seed & _MASK, offset & _MASK,
         to, _type(_FLOAT, dtype, "out"), old, st))
-    return out
+    _changed(out)
+    return looked_up
 
 
 def lookup_grad(tokens, grad, rows, scale=1.0, p=0.0, seed=0, offset=0, dtype=None, out=None,
@@ -179,13 +193,14 @@ def lookup_grad(tokens, grad, rows, scale=1.0, p=0.0, seed=0, offset=0, dtype=No
     if dtype is None:
         dtype = torch.float32 if out is None else out.dtype
     ws = _workspace(lib.sp_lookup_grad_workspace, grad.device, n, rows, dim)
-    out, to, old = _output(out, (rows, dim), dtype, grad.device)
+    total, to, old = _output(out, (rows, dim), dtype, grad.device)
     _check(lib.sp_lookup_grad(
         ids.data_ptr(), _type(_INDEX, tokens.dtype, "tokens"), n, g.data_ptr(),
         _type(_FLOAT, grad.dtype, "gradient"), dim, ld, scale, p, seed & _MASK, offset & _MASK,
         to, _type(_FLOAT, dtype, "out"), rows, old, 1 if accumulate else 0,
         *((0, 0) if ws is None else (ws.data_ptr(), ws.shape[0])), st))
-    return out
+    _changed(out)
+    return total
 
 
 def dropout(x, p, seed, offset=0, residual=None, out=None, stream=None):
@@ -202,13 +217,14 @@ def dropout(x, p, seed, offset=0, residual=None, out=None, stream=None):
         if residual.shape != x.shape or residual.dtype != x.dtype:
             raise _bad(f"x {tuple(x.shape)} {x.dtype}, residual {tuple(residual.shape)} {residual.dtype}")
         r, rld = _rows(residual, "residual")
-    out, to, old = _output(out, x.shape, x.dtype, x.device)
+    y, to, old = _output(out, x.shape, x.dtype, x.device)
     n, dim = v.shape
     if dim:
         _check((_lib or _load()).sp_dropout(
             v.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, ld, 0 if r is None else r.data_ptr(), rld,
             p, seed & _MASK, offset & _MASK, to, old, st))
-    return out
+        _changed(out)
+    return y
 
 
 def _stride(dim):
@@ -272,6 +288,7 @@ def cache_write(q, scales, x, slots, stream=None):
         r.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, rld, at.data_ptr(),
         _type(_INDEX, slots.dtype, "slots"), group, v.data_ptr(), _type(_KIND, q.dtype, "cache"), size, ld,
         s.data_ptr(), sld, st))
+    _changed((q, scales))
 
 
 def cache_read(q, scales, slots, dtype=torch.bfloat16, out=None, stream=None):
@@ -284,12 +301,13 @@ def cache_read(q, scales, slots, dtype=torch.bfloat16, out=None, stream=None):
     v, ld, s, sld, group = _cache(q, scales)
     at = _flat(slots)
     size, dim = v.shape
-    out, to, old = _output(out, (*slots.shape, dim), dtype, q.device)
+    rows, to, old = _output(out, (*slots.shape, dim), dtype, q.device)
     _check((_lib or _load()).sp_cache_read(
         v.data_ptr(), _type(_KIND, q.dtype, "cache"), size, dim, ld, s.data_ptr(), sld, group,
         at.data_ptr(), _type(_INDEX, slots.dtype, "slots"), at.shape[0], to,
         _type(_FLOAT, dtype, "out"), old, st))
-    return out
+    _changed(out)
+    return rows
 
 
 def quantize(x, group=None, dtype=torch.int8, stream=None):
@@ -334,9 +352,10 @@ def product(x, x_scales, w, w_scales, dtype=torch.bfloat16, out=None, stream=Non
     b, bld = _rows(w, "w")
     xs, ws = _flat(x_scales), _flat(w_scales)
     work = _workspace(lib.sp_product_workspace, x.device, m, n, k)
-    out, to, old = _output(out, (m, n), dtype, x.device)
+    scores, to, old = _output(out, (m, n), dtype, x.device)
     _check(lib.sp_product(
         a.data_ptr(), xs.data_ptr(), m, ald, b.data_ptr(), ws.data_ptr(), n, bld, k, to,
         _type(_FLOAT, dtype, "out"), old, *((0, 0) if work is None else (work.data_ptr(), work.shape[0])),
         st))
-    return out
+    _changed(out)
+    return scores
