@@ -369,7 +369,8 @@ void sp_host_free(void *ptr);
  * in 8 bits, read back (sp_cache_write, sp_cache_read) and scored against
  * (sp_product).  These calls take no context.  They enqueue kernels on `stream`
  * of the current device, allocate nothing, keep nothing, wait for nothing (so
- * they can be captured into a graph), and may be used from several threads.
+ * they can be captured into a graph; numbers given by value, seed and offset among
+ * them, are then those of the capture), and may be used from several threads.
  *
  *  - A matrix is a pointer, its element type and `ld`, the elements from the
  *    start of one row to the next (at least its columns); the elements of a row
@@ -423,6 +424,9 @@ sp_status sp_lookup_grad(const void *tokens, int32_t token_type, int64_t n, cons
  * is drawn from seed, offset and the element's row and column and stored nowhere:
  * the gradient to x is the same call on the output's gradient without a residual
  * (the residual's is the output's gradient itself).  Give every use its own offset.
+ * A captured call keeps its offset: every replay of the graph drops the same places, so
+ * a training step that is replayed has its dropout outside the graph, or a graph for
+ * each of several offsets.  The same holds for sp_lookup and sp_lookup_grad with p > 0.
  * The generator is Philox 4x32-10 with counter (column / 8, row, offset low, offset
  * high) and key (seed low, seed high); its four words are 16 bits for each of 8
  * columns, the low half of a word first; a column is dropped where they are below

@@ -206,7 +206,10 @@ def lookup_grad(tokens, grad, rows, scale=1.0, p=0.0, seed=0, offset=0, dtype=No
 def dropout(x, p, seed, offset=0, residual=None, out=None, stream=None):
     """[residual +] dropout of x, whose mask is drawn from (seed, offset) and each element's
     place and never stored.  Its gradient to x is dropout(grad, p, seed, offset), the
-    residual's is grad itself.  out may be x or residual."""
+    residual's is grad itself.  out may be x or residual.
+
+    Captured into a graph, the call keeps its seed and offset: every replay drops the same
+    places.  The same holds for lookup and lookup_grad with p > 0."""
     st = _stream(stream, x, (residual, out))
     if st is None:
         with _on(stream, x):
