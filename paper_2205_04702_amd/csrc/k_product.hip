@@ -17,6 +17,7 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 constexpr int KT = 64;      // bytes of a row in one step
 constexpr int STAGES = 4;   // steps that LDS holds
 constexpr int CHUNK = 16;   // bytes of one access
+constexpr uint32_t GROUP = 8;  // columns of tiles that an XCD works through together
 
 __device__ __forceinline__ void to_lds(const int8_t *src, int8_t *dst)
 {
@@ -78,22 +79,24 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs 
     constexpr int BUF = (BM + BN) * KT;
     __shared__ __attribute__((aligned(16))) int8_t sm[STAGES * BUF];
     const int wave = wave_id(), lane = lane_id();
-    // Which tile: each XCD takes a stretch of the tiles, in groups of four columns of tiles, so
-    // that what runs on it at a time (8 x 4 tiles, say, of 12 tiles' rows) shares its L2 and
-    // rows of w are read by one XCD.  Against tile after tile along a row of tiles, XCD after
-    // XCD (us, rows past the caches): 16384 x 2048 x 8192 250 and 274, x 2048 77 and 83,
-    // 1000 x 60000 x 4096 262 and 280, 5000 x 5000 x 5000 139 and 145, 3000 x 20000 x 2000 139 and
-    // 147; with 64 columns of tiles the other way round, 8192 x 16384 x 512 128 and 122, x 4096
-    // 512 and 507; in 23 more shapes, k from 300 to 8192, up to 7 % less or 4 % more.  One row of
-    // tiles has nothing to share, and the divisions' time to lose: 64 x 4096 x 4096 13.3 in
+    // Which tile: each XCD takes a stretch of the tiles, in groups of eight columns of tiles, so
+    // that what runs on it at a time (4 x 8 tiles, say, of 12 tiles' rows) shares its L2 and
+    // rows of w are read by one XCD.  Tile after tile along a row of tiles and XCD after XCD,
+    // groups of four columns, of eight, of sixteen (us, rows past the caches):
+    //   8192 x 16384 x 512      125  134  126  135       5000 x 5000 x 5000    150  141  147  144
+    //   8192 x 16384 x 4096     518  524  521  528       16384 x 2048 x 8192   266  250  250  250
+    //   10000 x 30000 x 1000    444  418  398  429       1000 x 60000 x 4096   286  260  263  264
+    //   6000 x 12000 x 3000     249  234  233  239       3000 x 20000 x 300     60   57   54   53
+    // and within 2 % of the best of them in 17 more shapes, in 5000 x 5000 x 2500 within 4 %.  One row
+    // of tiles has nothing to share, and the divisions' time to lose: 64 x 4096 x 4096 13.3 in
     // groups, 12.5 without.
     uint32_t tile_m = 0, tile_n = blockIdx.x;
     if (tiles_m > 1) {
         const uint32_t tile = (uint32_t)xcd_block(blockIdx.x, gridDim.x);
-        const uint32_t group = tile / (4u * tiles_m), in = tile - group * 4u * tiles_m;
-        const uint32_t wide = (uint32_t)tiles_n - group * 4u < 4u ? (uint32_t)tiles_n - group * 4u : 4u;
+        const uint32_t group = tile / (GROUP * tiles_m), in = tile - group * GROUP * tiles_m;
+        const uint32_t wide = (uint32_t)tiles_n - group * GROUP < GROUP ? (uint32_t)tiles_n - group * GROUP : GROUP;
         tile_m = in / wide;
-        tile_n = group * 4u + in % wide;
+        tile_n = group * GROUP + in % wide;
     }
     const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
     constexpr bool PARTIAL = std::is_same<TO, int32_t>::value;  // sums of a part of k
