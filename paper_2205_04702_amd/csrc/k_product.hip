@@ -65,9 +65,9 @@ __device__ __forceinline__ v4i short_row(const int8_t *row, int32_t at, int32_t 
 // factor of the matrix instruction: its four consecutive rows per lane are four
 // consecutive outputs of a row.
 //
-// 8192^3 in tiles of 256: 466 to 473 us, 2.3 to 2.4 POP/s, at the clock that power leaves (1.5 GHz by
-// the counters; matrix instructions alone took 368 us), the matrix cores busy two thirds
-// of the time.  What a CU loads bounds smaller tiles: 12 to 13 TB/s from L2 together.
+// 8192^3 in tiles of 256: 480 to 500 us, 2.2 to 2.3 POP/s, at the clock that power leaves (1.65 GHz
+// by the counters; matrix instructions alone took 368 us), the matrix cores busy 65 % of the time,
+// 89 % of the reads served by L2.  Smaller tiles are bound by what a CU loads.
 template <int BM, int BN, int WM, int WN, typename TO, bool ALIGNED>
 __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product(ProductArgs a, int32_t tiles_n, uint32_t tiles_m, int32_t per_split)
 {

@@ -8,8 +8,10 @@ namespace sp {
 // out[i] = factor * keep(i) * table[token[i]], rows of zeros where the token is
 // no row of the table (padding).  A thread has its octet of one row: its token, then its
 // columns, of four rows at a time where there are many.  Bound by the bytes: 16384 rows of
-// 2048 in bf16 with dropout 18 us (67 MB written, 27 MB of distinct rows read; 131072 random rows of
-// 2048 without 245 us, 4.4 TB/s).  Outputs go past the caches there, the table does not: tokens repeat.
+// 2048 in bf16 with dropout 20 us (67 MB written, 27 MB of distinct rows read; 17.5 a call with
+// the rows in the caches from the call before, 23.6 with other tables in between; 131072 random
+// rows of 2048 without 245 us, 4.4 TB/s).  Outputs go past the caches there, the table does not:
+// tokens repeat.
 template <typename TI, typename TO, typename IX, bool DROP>
 struct Lookup {
     static constexpr bool DEEP = true;
