@@ -363,11 +363,12 @@ void sp_host_free(void *ptr);
 
 /*
  * ---------------------------------------------------------------------------
- * Operators on token tables and 8-bit rows, on device memory.
+ * Operators on token tables, rows in 8 and 4 bits and scores, on device memory.
  *
- * A table of rows is trained (sp_lookup, sp_lookup_grad, sp_dropout), then kept
+ * A table of rows is trained (sp_lookup, sp_lookup_grad, sp_dropout, sp_distill_grad), then kept
  * in 8 bits, read back (sp_cache_write, sp_cache_read) and scored against
- * (sp_product).  These calls take no context.  They enqueue kernels on `stream`
+ * (sp_product), or in 4 bits (sp_cache4_write, sp_cache4_read, sp_product4); scores are adjusted
+ * before tokens are chosen from them (sp_adjust).  These calls take no context.  They enqueue kernels on `stream`
  * of the current device, allocate nothing, keep nothing, wait for nothing (so
  * they can be captured into a graph; numbers given by value, seed and offset among
  * them, are then those of the capture), and may be used from several threads.
@@ -479,6 +480,99 @@ sp_status sp_product(const int8_t *x, const float *x_scales, int64_t m, int64_t 
                      const int8_t *w, const float *w_scales, int64_t n, int64_t w_ld, int64_t k,
                      void *out, int32_t out_type, int64_t out_ld, void *workspace,
                      int64_t workspace_bytes, void *stream);
+
+/*
+ * A cache of rows in 4 bits: q [slots][dim / 32 * 16] bytes and scales [slots][dim / 32] bytes,
+ * dim rounded up to a multiple of 32.  Blocks of 32 columns share a scale 2^(byte - 127); a value is
+ * scale times 0, .5, 1, 1.5, 2, 3, 4 or 6, its code (0 .. 7, the sign in bit 3) in half a byte, the
+ * even column's in the low half: the MXFP4 format of the OCP Microscaling Formats specification.
+ *
+ * sp_cache4_write quantises row i of x (SP_F32, SP_BF16 or SP_F16) into slot index[i] (SP_I32 or
+ * SP_I64; NULL: slot i).  With a the block's largest magnitude, scale = 2^(floor(log2 a) - 2), 2^-127
+ * at least; code = x / scale rounded to nearest, ties to even codes, above 6 to 6.  Everything but
+ * that rounding is exact.  A block with an infinity or NaN gets the byte 255 and reads back as NaN.
+ * Columns past dim in the last block are written as zeros.  Rows whose index is no slot are left
+ * out.  The slots of one call are distinct, as for sp_cache_write.
+ *
+ * sp_cache4_read gives the values of slot index[i], zeros where the index is no slot.
+ */
+sp_status sp_cache4_write(const void *x, int32_t type, int64_t n, int64_t dim, int64_t x_ld,
+                          const void *index, int32_t index_type, uint8_t *q, int64_t slots,
+                          int64_t q_ld, uint8_t *scales, int64_t scales_ld, void *stream);
+sp_status sp_cache4_read(const uint8_t *q, int64_t slots, int64_t dim, int64_t q_ld,
+                         const uint8_t *scales, int64_t scales_ld, const void *index,
+                         int32_t index_type, int64_t n, void *out, int32_t out_type, int64_t out_ld,
+                         void *stream);
+
+/*
+ * out[i][j] = sum over c < k of x[i][c] * w[j][c], i < m, j < n, of rows in 4 bits (k: 1 .. 2^20,
+ * rounded up to a multiple of 32: what the last block holds past k counts, so zeros).  Products and
+ * scales are exact, sums fp32.  A scale byte of 255 gives NaN.  Rows of x, of w and of their scales
+ * start at multiples of 16 bytes (x and w best of 128), and are read in whole aligned 16-byte
+ * pieces (scales past the row's last count nothing); strides of x and w are below 2^23.
+ * out: SP_F32, SP_BF16 or SP_F16.  workspace: as for sp_lookup_grad, of the bytes that
+ * sp_product4_workspace gives for m, n and k.
+ */
+sp_status sp_product4_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes);
+sp_status sp_product4(const uint8_t *x, const uint8_t *x_scales, int64_t m, int64_t x_ld,
+                      int64_t x_scales_ld, const uint8_t *w, const uint8_t *w_scales, int64_t n,
+                      int64_t w_ld, int64_t w_scales_ld, int64_t k, void *out, int32_t out_type,
+                      int64_t out_ld, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Scores [n][vocab] adjusted before a token is chosen, row by row: for a column v that is c > 0 times
+ * among the row's previous tokens
+ *     y = (s > 0 ? s / repetition : s * repetition) - (presence + frequency * c),   else y = s;
+ * plus the bias of v (of several entries for v the last); -infinity where v is not allowed,
+ * whatever s holds.  scores and out have one type (SP_F32, SP_BF16 or SP_F16); out may be scores
+ * itself (same pointer and ld).
+ *   previous [n][length], SP_I32 or SP_I64: tokens outside 0 .. vocab-1 (padding) count nothing;
+ *     length 0: none.
+ *   penalties [n][3] fp32: each row's repetition, presence and frequency in place of the numbers
+ *     (NULL: the numbers, repetition positive, all finite).
+ *   bias_tokens [n][biases], SP_I32 or SP_I64, and bias [n][biases] fp32: entries whose token is
+ *     no column count nothing; biases 0: none.
+ *   allowed [n][vocab / 32, rounded up]: column v is bit v % 32 of word v / 32 (NULL: all).
+ * Strides of these four may be 0: one row for all.  vocab, length and biases: at most 2^20.
+ */
+sp_status sp_adjust(const void *scores, int32_t type, int64_t n, int64_t vocab, int64_t ld,
+                    const void *previous, int32_t previous_type, int64_t length, int64_t previous_ld,
+                    float repetition, float presence, float frequency, const float *penalties,
+                    int64_t penalties_ld, const void *bias_tokens, int32_t bias_type,
+                    int64_t bias_tokens_ld, const float *bias, int64_t bias_ld, int64_t biases,
+                    const int32_t *allowed, int64_t allowed_ld, void *out, int64_t out_ld,
+                    void *stream);
+
+/*
+ * Distillation of scores [n][vocab] (SP_F32, SP_BF16 or SP_F16) from a teacher's top logits:
+ * tokens [n][k] (SP_I32 or SP_I64) and teacher [n][k] (SP_F32, SP_BF16 or SP_F16), k 1 .. 1024.
+ * With T the temperature, p the softmax of teacher / T over the row's entries and q that of
+ * scores / T over its columns,
+ *     loss[i] = T^2 * sum over entries j of p_j * (log p_j - log q_token(j)).
+ * Entries whose token is no column (padding) are none; a token listed several times counts as often.
+ * A row without entries, or with none above -infinity, has loss 0, whatever its scores hold.
+ * Entries with p = 0 count nothing; a score of -infinity under p > 0 gives a loss of infinity (a row
+ * of them alone: q = 0 everywhere), NaN and +infinity a loss of NaN or infinity.
+ *
+ * sp_distill_grad gives the loss and the gradient of weight * loss[i] to the scores,
+ *     grad[i][v] = weight * T * (q_v - sum over j with token(j) = v of p_j),
+ * zeros for a row of loss 0 by lack of entries.  weights [n] fp32: each row's in place of the number
+ * (NULL: the number).  grad: SP_F32, SP_BF16 or SP_F16; it may be scores itself (same pointer,
+ * type and ld).
+ * workspace: as for sp_lookup_grad, of the bytes that sp_distill_workspace gives for n, vocab, k and
+ * whether the gradient is asked for.
+ */
+sp_status sp_distill_workspace(int64_t n, int64_t vocab, int64_t k, int32_t grad, int64_t *bytes);
+sp_status sp_distill(const void *scores, int32_t type, int64_t n, int64_t vocab, int64_t ld,
+                     const void *tokens, int32_t token_type, int64_t tokens_ld, const void *teacher,
+                     int32_t teacher_type, int64_t teacher_ld, int64_t k, float temperature,
+                     float *loss, void *workspace, int64_t workspace_bytes, void *stream);
+sp_status sp_distill_grad(const void *scores, int32_t type, int64_t n, int64_t vocab, int64_t ld,
+                          const void *tokens, int32_t token_type, int64_t tokens_ld,
+                          const void *teacher, int32_t teacher_type, int64_t teacher_ld, int64_t k,
+                          float temperature, float weight, const float *weights, float *loss,
+                          void *grad, int32_t grad_type, int64_t grad_ld, void *workspace,
+                          int64_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

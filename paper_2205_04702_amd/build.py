@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libscratchpipe.so")
 SOURCES = ["k_ingest.hip", "k_plan.hip", "k_train.hip", "k_tokens.hip", "k_tokengrad.hip",
-           "k_cache.hip", "k_product.hip", "capi.cpp", "rowapi.cpp"]
+           "k_cache.hip", "k_product.hip", "k_cache4.hip", "k_product4.hip", "k_adjust.hip",
+           "k_distill.hip", "capi.cpp", "rowapi.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

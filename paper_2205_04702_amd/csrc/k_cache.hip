@@ -62,58 +62,6 @@ __device__ __forceinline__ void unpack_oct(const uint32_t (&x)[2], float (&v)[OC
     }
 }
 
-// The largest magnitude's bits in an octet as loaded, of its first `valid` columns: for
-// 16-bit types the larger of two at a time, in the high or low half.
-typedef uint16_t half_2 __attribute__((ext_vector_type(2)));
-template <typename T>
-__device__ __forceinline__ uint32_t top_of(const Raw<T> &r, int valid)
-{
-    uint32_t m = 0;
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int k = 0; k < OCT; ++k) {
-            const uint32_t b = r.w[k] & 0x7FFFFFFFu;
-            m = k < valid && b > m ? b : m;
-        }
-    } else {
-        half_2 t = {0, 0};
-#pragma unroll
-        for (int i = 0; i < OCT / 2; ++i) {
-            const int left = valid - 2 * i;
-            uint32_t b = r.w[i] & (left >= 2 ? 0x7FFF7FFFu : left == 1 ? 0x7FFFu : 0u);
-            half_2 h;
-            __builtin_memcpy(&h, &b, 4);
-            t = __builtin_elementwise_max(t, h);
-        }
-        m = t.x > t.y ? t.x : t.y;
-    }
-    return m;
-}
-// ... as the bits of a float.
-template <typename T>
-__device__ __forceinline__ uint32_t float_bits(uint32_t m)
-{
-    if constexpr (sizeof(T) == 4) return m;
-    Raw<T> r;
-    r.w[0] = m;
-    return __float_as_uint(raw_float(r, 0));
-}
-
-// The maximum over each TEAM lanes, in all of them: exchanges inside rows of 16 lanes, then
-// between them.
-template <int TEAM>
-__device__ __forceinline__ uint32_t team_max(uint32_t m)
-{
-    const auto with = [&](uint32_t o) { m = o > m ? o : m; };
-    if constexpr (TEAM >= 2) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true));   // lane ^ 1
-    if constexpr (TEAM >= 4) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));   // lane ^ 2
-    if constexpr (TEAM >= 8) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xF, 0xF, true));  // the other four of eight
-    if constexpr (TEAM >= 16) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x140, 0xF, 0xF, true)); // the other eight
-    if constexpr (TEAM >= 32) with((uint32_t)__shfl_xor((int)m, 16, WAVE));
-    if constexpr (TEAM >= 64) with((uint32_t)__shfl_xor((int)m, 32, WAVE));
-    return m;
-}
-
 __device__ __forceinline__ void store_bytes(uint8_t *p, int valid, uint2 w)
 {
     if (valid >= OCT) {

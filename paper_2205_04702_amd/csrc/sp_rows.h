@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "sp_device.h"
 
 namespace sp {
@@ -183,6 +185,58 @@ __device__ __forceinline__ void store_oct(T *p, int valid, const float (&v)[OCT]
         for (int k = 0; k < OCT; ++k)
             if (k < valid) p[k] = from_float<T>(v[k]);
     }
+}
+
+// The largest magnitude's bits in an octet as loaded, of its first `valid` columns: for
+// 16-bit types the larger of two at a time, in the high or low half.
+typedef uint16_t half_2 __attribute__((ext_vector_type(2)));
+template <typename T>
+__device__ __forceinline__ uint32_t top_of(const Raw<T> &r, int valid)
+{
+    uint32_t m = 0;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < OCT; ++k) {
+            const uint32_t b = r.w[k] & 0x7FFFFFFFu;
+            m = k < valid && b > m ? b : m;
+        }
+    } else {
+        half_2 t = {0, 0};
+#pragma unroll
+        for (int i = 0; i < OCT / 2; ++i) {
+            const int left = valid - 2 * i;
+            uint32_t b = r.w[i] & (left >= 2 ? 0x7FFF7FFFu : left == 1 ? 0x7FFFu : 0u);
+            half_2 h;
+            __builtin_memcpy(&h, &b, 4);
+            t = __builtin_elementwise_max(t, h);
+        }
+        m = t.x > t.y ? t.x : t.y;
+    }
+    return m;
+}
+// ... as the bits of a float.
+template <typename T>
+__device__ __forceinline__ uint32_t float_bits(uint32_t m)
+{
+    if constexpr (sizeof(T) == 4) return m;
+    Raw<T> r;
+    r.w[0] = m;
+    return __float_as_uint(raw_float(r, 0));
+}
+
+// The maximum over each TEAM lanes, in all of them: exchanges inside rows of 16 lanes, then
+// between them.
+template <int TEAM>
+__device__ __forceinline__ uint32_t team_max(uint32_t m)
+{
+    const auto with = [&](uint32_t o) { m = o > m ? o : m; };
+    if constexpr (TEAM >= 2) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true));   // lane ^ 1
+    if constexpr (TEAM >= 4) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));   // lane ^ 2
+    if constexpr (TEAM >= 8) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xF, 0xF, true));  // the other four of eight
+    if constexpr (TEAM >= 16) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x140, 0xF, 0xF, true)); // the other eight
+    if constexpr (TEAM >= 32) with((uint32_t)__shfl_xor((int)m, 16, WAVE));
+    if constexpr (TEAM >= 64) with((uint32_t)__shfl_xor((int)m, 32, WAVE));
+    return m;
 }
 
 // The value that lane CTRL's two bits for this lane name, among each four lanes.
@@ -402,6 +456,22 @@ inline hipError_t with_index(int32_t type, F f)
     return type == 3 ? f(int32_t()) : f(int64_t());
 }
 
+// Element `at` of an array whose type is known at run time.
+__device__ __forceinline__ int64_t index_at(const void *p, int32_t type, int64_t at)
+{
+    return type == 3 ? (int64_t)((const int32_t *)p)[at] : ((const int64_t *)p)[at];
+}
+__device__ __forceinline__ float float_at(const void *p, int32_t type, int64_t at)
+{
+    return type == 0   ? ((const float *)p)[at]
+           : type == 1 ? to_float(((const __bf16 *)p)[at])
+                       : to_float(((const _Float16 *)p)[at]);
+}
+inline const void *index_past(const void *p, int32_t type, int64_t by)
+{
+    return p ? (const char *)p + by * (type == 3 ? 4 : 8) : nullptr;
+}
+
 // ---------------------------------------------------------------- host entry of each operator
 
 struct LookupArgs {
@@ -469,6 +539,22 @@ struct CacheArgs {
 hipError_t run_cache_write(const CacheArgs &a, hipStream_t s);
 hipError_t run_cache_read(const CacheArgs &a, hipStream_t s);
 
+struct Cache4Args {
+    const void *index;  // null: row i is slot i
+    int32_t index_type;
+    int64_t n;
+    uint8_t *q;
+    int64_t slots, q_ld;
+    uint8_t *scales;
+    int64_t scales_ld;
+    int32_t dim;
+    void *x;  // the rows written, or read
+    int32_t type;
+    int64_t x_ld;
+};
+hipError_t run_cache4_write(const Cache4Args &a, hipStream_t s);
+hipError_t run_cache4_read(const Cache4Args &a, hipStream_t s);
+
 struct ProductArgs {
     const int8_t *x, *w;
     const float *xs, *ws;
@@ -480,7 +566,70 @@ struct ProductArgs {
     int64_t out_ld;
     char *work;
 };
+struct Cut {
+    int32_t tile, splits;
+};
+Cut cut_product(int64_t m, int64_t n, int64_t bytes);  // rows of so many bytes
 int64_t product_workspace(int64_t m, int64_t n, int64_t k);
 hipError_t run_product(const ProductArgs &a, hipStream_t s);
+
+struct Product4Args {
+    const uint8_t *x, *xs, *w, *ws;  // rows of bytes, rows of scales
+    int64_t m, n;
+    int32_t blocks;  // of 32 columns, in a row
+    int64_t x_ld, xs_ld, w_ld, ws_ld;
+    void *out;
+    int32_t out_type;
+    int64_t out_ld;
+    char *work;
+};
+int64_t product4_workspace(int64_t m, int64_t n, int32_t blocks);
+hipError_t run_product4(const Product4Args &a, hipStream_t s);
+
+struct AdjustArgs {
+    const void *scores;
+    int32_t type;
+    int64_t n, ld;
+    int32_t vocab;
+    const void *previous;  // null: none
+    int32_t previous_type, length;
+    int64_t previous_ld;
+    float repetition, presence, frequency;
+    const float *penalties;  // null: the three numbers
+    int64_t penalties_ld;
+    const void *bias_tokens;  // null: none
+    int32_t bias_type, biases;
+    int64_t bias_tokens_ld;
+    const float *bias;
+    int64_t bias_ld;
+    const uint8_t *allowed;  // null: every token
+    int64_t allowed_ld;      // bytes
+    void *out;
+    int64_t out_ld;
+};
+hipError_t run_adjust(const AdjustArgs &a, hipStream_t s);
+
+struct DistillArgs {
+    const void *scores;
+    int32_t type;
+    int64_t n, ld;
+    int32_t vocab, k;
+    const void *tokens;
+    int32_t token_type;
+    int64_t tokens_ld;
+    const void *teacher;
+    int32_t teacher_type;
+    int64_t teacher_ld;
+    float temperature;
+    float *loss;
+    const float *weights;  // null: weight
+    float weight;
+    void *grad;  // null: the loss alone
+    int32_t grad_type;
+    int64_t grad_ld;
+    char *work;
+};
+int64_t distill_workspace(int64_t n, int32_t vocab, int32_t k, bool grad);
+hipError_t run_distill(const DistillArgs &a, hipStream_t s);
 
 }  // namespace sp

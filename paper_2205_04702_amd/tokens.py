@@ -1,4 +1,4 @@
-"""Operators on token tables and 8-bit rows (include/scratchpipe.h, second part).
+"""Operators on token tables, rows in 8 and 4 bits and scores (include/scratchpipe.h, second part).
 
 Argument marshalling only, as in scratchpipe.py: torch tensors on the GPU in, kernels
 of the HIP library on the current stream (or the one given), torch tensors out.
@@ -9,6 +9,10 @@ of the HIP library on the current stream (or the one given), torch tensors out.
     q, scales = quantize(table)                                 # serving: rows in 8 bits
     cache_write(q, scales, x, slots); x = cache_read(q, scales, slots)
     scores = product(*quantize(x), q, scales)
+    q, scales = quantize4(table)                                # serving: rows in 4 bits
+    scores = product4(*quantize4(x), q, scales)
+    scores = adjust(scores, previous, repetition=1.1, allowed=words)  # before a token is chosen
+    loss, grad = distill_grad(scores, top_tokens, top_logits, weight=1 / n)  # training
 
 Autograd does not see these calls: what they return requires no gradient even where an input
 does, and gradients are taken by calls of their own (lookup_grad; dropout on the gradient).
@@ -19,6 +23,7 @@ has to be ready there, and to stay allocated until it is done.
 from __future__ import annotations
 
 import ctypes as C
+import math
 
 import torch
 from torch.autograd.graph import increment_version
@@ -29,6 +34,7 @@ SP_F32, SP_BF16, SP_F16, SP_I32, SP_I64, SP_I8, SP_F8 = range(7)  # the header's
 _FLOAT = {torch.float32: SP_F32, torch.bfloat16: SP_BF16, torch.float16: SP_F16}
 _INDEX = {torch.int32: SP_I32, torch.int64: SP_I64}
 _KIND = {torch.int8: SP_I8, torch.float8_e4m3fn: SP_F8}
+_F32, _I32 = {torch.float32: SP_F32}, {torch.int32: SP_I32}
 _MASK = (1 << 64) - 1
 
 # (the public forms build objects: torch.cuda.current_stream().cuda_stream takes 1 us)
@@ -50,7 +56,15 @@ def _load():
                 ("sp_cache_write", [p, i, l, l, l, p, i, l, p, i, l, l, p, l, p]),
                 ("sp_cache_read", [p, i, l, l, l, p, l, l, p, i, l, p, i, l, p]),
                 ("sp_product_workspace", [l, l, l, C.POINTER(l)]),
-                ("sp_product", [p, p, l, l, p, p, l, l, l, p, i, l, p, l, p])):
+                ("sp_product", [p, p, l, l, p, p, l, l, l, p, i, l, p, l, p]),
+                ("sp_cache4_write", [p, i, l, l, l, p, i, p, l, l, p, l, p]),
+                ("sp_cache4_read", [p, l, l, l, p, l, p, i, l, p, i, l, p]),
+                ("sp_product4_workspace", [l, l, l, C.POINTER(l)]),
+                ("sp_product4", [p, p, l, l, l, p, p, l, l, l, l, p, i, l, p, l, p]),
+                ("sp_adjust", [p, i, l, l, l, p, i, l, l, f, f, f, p, l, p, i, l, p, l, l, p, l, p, l, p]),
+                ("sp_distill_workspace", [l, l, l, i, C.POINTER(l)]),
+                ("sp_distill", [p, i, l, l, l, p, i, l, p, i, l, l, f, p, p, l, p]),
+                ("sp_distill_grad", [p, i, l, l, l, p, i, l, p, i, l, l, f, f, p, p, p, i, l, p, l, p])):
             fn = getattr(L, name)
             fn.argtypes, fn.restype = args, i
         _lib = L
@@ -362,3 +376,255 @@ def product(x, x_scales, w, w_scales, dtype=torch.bfloat16, out=None, stream=Non
         st))
     _changed(out)
     return scores
+
+
+# ------------------------------------------------------------------ rows in 4 bits
+
+def _blocks(dim):
+    if dim < 1:
+        raise _bad(f"rows of {dim} columns")
+    return (dim + 31) // 32
+
+
+def _strides4(dim):
+    """Bytes from row to row of 4-bit rows, as _stride, and of their scales, which product4()
+    reads in whole 16-byte pieces."""
+    return _stride(_blocks(dim) * 16), (_blocks(dim) + 15) // 16 * 16
+
+
+def empty_cache4(slots, dim, device="cuda"):
+    """Bytes [slots, dim / 2] and scales [slots, dim / 32] (uint8, dim rounded up to a multiple of
+    32) of a cache of rows in 4 bits, all zeros, laid out as product4() needs them."""
+    blocks, (ld, sld) = _blocks(dim), _strides4(dim)
+    q = torch.zeros((slots, ld), dtype=torch.uint8, device=device)[:, :blocks * 16]
+    return q, torch.zeros((slots, sld), dtype=torch.uint8, device=device)[:, :blocks]
+
+
+def _shapes4(q, scales, dim, what):
+    if q.dim() != 2 or scales.dim() != 2 or q.dtype != torch.uint8 or scales.dtype != torch.uint8 \
+            or scales.shape[0] != q.shape[0] or q.shape[1] != 16 * scales.shape[1] or not scales.shape[1]:
+        raise _bad(f"{what} {tuple(q.shape)} {q.dtype}, scales {tuple(scales.shape)} {scales.dtype}: uint8 "
+                   "[rows, dim / 2] and [rows, dim / 32] are needed, dim a multiple of 32")
+    if dim is not None and scales.shape[1] != _blocks(dim):
+        raise _bad(f"{what}: {scales.shape[1]} scales per row, {_blocks(dim)} are needed for {dim} columns")
+
+
+def _cache4(q, scales, dim):
+    """Bytes, their row stride, scales, theirs."""
+    _shapes4(q, scales, dim, "cache")
+    v, ld = _rows(q, "cache", copy=False)
+    s, sld = _rows(scales, "scales", copy=False)
+    return v, ld, s, sld
+
+
+def cache_write4(q, scales, x, slots, stream=None):
+    """Quantises the rows of x [*slots.shape, dim] (dim may be several dimensions) to 4 bits, into
+    the given slots (distinct; rows of a slot outside the cache, as -1, are left out)."""
+    st = _stream(stream, q, (scales, x, slots))
+    if st is None:
+        with _on(stream, q):
+            return cache_write4(q, scales, x, slots)
+    if x.shape[:slots.dim()] != slots.shape:
+        raise _bad(f"{tuple(slots.shape)} slots, rows {tuple(x.shape)}")
+    at = _flat(slots)
+    n, dim = at.shape[0], math.prod(x.shape[slots.dim():])
+    v, ld, s, sld = _cache4(q, scales, dim)
+    r = x
+    if x.dim() != 2 or slots.dim() != 1:
+        try:
+            r = x.view(n, dim)
+        except RuntimeError:
+            r = x.reshape(n, dim)
+    r, rld = _rows(r, "x")
+    _check((_lib or _load()).sp_cache4_write(
+        r.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, rld, at.data_ptr(), _type(_INDEX, slots.dtype, "slots"),
+        v.data_ptr(), v.shape[0], ld, s.data_ptr(), sld, st))
+    _changed((q, scales))
+
+
+def cache_read4(q, scales, slots, dim=None, dtype=torch.bfloat16, out=None, stream=None):
+    """The rows [*slots.shape, dim] that the given slots stand for; zeros for a slot outside the
+    cache (as -1).  dim: the columns of a row (default: all of its blocks')."""
+    st = _stream(stream, q, (scales, slots, out))
+    if st is None:
+        with _on(stream, q):
+            return cache_read4(q, scales, slots, dim, dtype, out)
+    v, ld, s, sld = _cache4(q, scales, dim)
+    if dim is None:
+        dim = 32 * s.shape[1]
+    at = _flat(slots)
+    rows, to, old = _output(out, (*slots.shape, dim), dtype, q.device)
+    _check((_lib or _load()).sp_cache4_read(
+        v.data_ptr(), v.shape[0], dim, ld, s.data_ptr(), sld, at.data_ptr(), _type(_INDEX, slots.dtype, "slots"),
+        at.shape[0], to, _type(_FLOAT, dtype, "out"), old, st))
+    _changed(out)
+    return rows
+
+
+def quantize4(x, stream=None):
+    """The rows of x [..., dim] in 4 bits: bytes [n, dim / 2] and scales [n, dim / 32] (dim rounded
+    up to a multiple of 32), laid out as empty_cache4() does."""
+    st = _stream(stream, x, ())
+    if st is None:
+        with _on(stream, x):
+            return quantize4(x)
+    r, rld = _rows(x, "x")
+    n, dim = r.shape
+    blocks, (ld, sld) = _blocks(dim), _strides4(dim)
+    q = torch.empty((n, ld), dtype=torch.uint8, device=x.device)
+    scales = torch.empty((n, sld), dtype=torch.uint8, device=x.device)
+    _check((_lib or _load()).sp_cache4_write(
+        r.data_ptr(), _type(_FLOAT, x.dtype, "x"), n, dim, rld, 0, 0, q.data_ptr(), n, ld, scales.data_ptr(), sld,
+        st))
+    return (q if ld == blocks * 16 else q[:, :blocks * 16]), (scales if sld == blocks else scales[:, :blocks])
+
+
+def _factor4(q, scales, what):
+    """A factor of product4, copied where its rows do not lie as the kernel reads them: bytes, their row
+    stride, scales, theirs."""
+    _shapes4(q, scales, None, what)
+    n, given = q.shape[0], []
+    for t, ld, most in zip((q, scales), _strides4(2 * q.shape[1]), (1 << 23, 1 << 40)):
+        width = t.shape[1]
+        if t.data_ptr() % 16 or (width > 1 and t.stride(1) != 1) or (
+                n > 1 and not (width <= t.stride(0) < most and t.stride(0) % 16 == 0)):
+            t = torch.empty((n, ld), dtype=torch.uint8, device=t.device)[:, :width].copy_(t)
+        given += [t, t.stride(0) if n > 1 else ld]
+    return given
+
+
+def product4(x, x_scales, w, w_scales, dtype=torch.bfloat16, out=None, stream=None):
+    """x @ w.T of rows in 4 bits, x [m, k / 2] and w [n, k / 2] bytes with their scales [m, k / 32] and
+    [n, k / 32], summed in fp32.  Rows that do not start at multiples of 16 bytes are copied first;
+    quantize4() and empty_cache4() give rows that do."""
+    st = _stream(stream, x, (x_scales, w, w_scales, out))
+    if st is None:
+        with _on(stream, x):
+            return product4(x, x_scales, w, w_scales, dtype, out)
+    a, ald, xs, xsld = _factor4(x, x_scales, "x")
+    b, bld, ws, wsld = _factor4(w, w_scales, "w")
+    if a.shape[1] != b.shape[1]:
+        raise _bad(f"x {tuple(x.shape)}, w {tuple(w.shape)}: [m, k / 2] and [n, k / 2] are needed")
+    lib = _lib or _load()
+    m, n, k = a.shape[0], b.shape[0], 2 * a.shape[1]
+    work = _workspace(lib.sp_product4_workspace, x.device, m, n, k)
+    scores, to, old = _output(out, (m, n), dtype, x.device)
+    _check(lib.sp_product4(
+        a.data_ptr(), xs.data_ptr(), m, ald, xsld, b.data_ptr(), ws.data_ptr(), n, bld, wsld, k, to,
+        _type(_FLOAT, dtype, "out"), old, *((0, 0) if work is None else (work.data_ptr(), work.shape[0])), st))
+    _changed(out)
+    return scores
+
+
+# ------------------------------------------------------------------ scores
+
+def _each_row(t, scores, width, what, dtypes):
+    """What a call has for each row of scores, [*rows, width], or for all of them alike, [width]: the
+    tensor, its address, its row stride (0: one row for all) and the number of its type."""
+    code = _type(dtypes, t.dtype, what)
+    if t.dim() == 0 or (t.dim() > 1 and t.shape[:-1] != scores.shape[:-1]) or (width is not None and t.shape[-1] != width):
+        raise _bad(f"{what} {tuple(t.shape)}, scores {tuple(scores.shape)}")
+    if t.dim() == 1:
+        t = _flat(t)
+        return t, t.data_ptr(), 0, code
+    t, ld = _rows(t, what)
+    return t, t.data_ptr(), ld, code
+
+
+def adjust(scores, previous=None, repetition=1.0, presence=0.0, frequency=0.0, penalties=None,
+           bias_tokens=None, bias=None, allowed=None, out=None, stream=None):
+    """Scores [..., vocab] adjusted before a token is chosen from them.
+
+    A column that is c > 0 times among the row's previous tokens: its score divided by repetition where
+    positive, else multiplied by it, less presence + frequency * c.  Then the bias of each column that
+    has one (of several entries the last).  Then -infinity where a column is not allowed.
+
+    previous: tokens [..., length], those outside the columns (padding, -1) count nothing.
+    penalties: float32 [..., 3], each row's repetition, presence and frequency in place of the
+    numbers.  bias_tokens, bias: tokens [..., entries] (padding as above) and their float32 biases.
+    allowed: int32 words [..., vocab / 32, rounded up], column v is bit v % 32 of word v / 32.  Each
+    of these may be [..., width] with the leading dimensions of scores, or [width] for all rows.
+    out may be scores."""
+    st = _stream(stream, scores, (previous, penalties, bias_tokens, bias, allowed, out))
+    if st is None:
+        with _on(stream, scores):
+            return adjust(scores, previous, repetition, presence, frequency, penalties, bias_tokens, bias, allowed, out)
+    if (bias_tokens is None) != (bias is None):
+        raise _bad("bias_tokens and bias come together")
+    x, ld = _rows(scores, "scores")
+    n, vocab = x.shape
+    code = _type(_FLOAT, scores.dtype, "scores")
+    none = (None, 0, 0, SP_I32)
+    prev = none if previous is None else _each_row(previous, scores, None, "previous", _INDEX)
+    pens = none if penalties is None else _each_row(penalties, scores, 3, "penalties", _F32)
+    btok = none if bias is None else _each_row(bias_tokens, scores, None, "bias_tokens", _INDEX)
+    entries = 0 if bias is None else bias_tokens.shape[-1]
+    bias_ = none if bias is None else _each_row(bias, scores, entries, "bias", _F32)
+    mask = none if allowed is None else _each_row(allowed, scores, (vocab + 31) // 32, "allowed", _I32)
+    y, to, old = _output(out, scores.shape, scores.dtype, scores.device)
+    if vocab:
+        _check((_lib or _load()).sp_adjust(
+            x.data_ptr(), code, n, vocab, ld, prev[1], prev[3], 0 if previous is None else previous.shape[-1], prev[2],
+            repetition, presence, frequency, pens[1], pens[2], btok[1], btok[3], btok[2], bias_[1], bias_[2], entries,
+            mask[1], mask[2], to, old, st))
+        _changed(out)
+    return y
+
+
+def _distilled(scores, tokens, teacher):
+    """The arguments that distill and distill_grad share, and what keeps their copies alive."""
+    if tokens.shape != teacher.shape or tokens.dim() == 0 or tokens.shape[:-1] != scores.shape[:-1]:
+        raise _bad(f"scores {tuple(scores.shape)}, tokens {tuple(tokens.shape)}, teacher {tuple(teacher.shape)}")
+    x, ld = _rows(scores, "scores")
+    tok, tld = _rows(tokens, "tokens")
+    t, eld = _rows(teacher, "teacher")
+    (n, vocab), k = x.shape, tokens.shape[-1]
+    return (x, tok, t), (n, vocab, k), (
+        x.data_ptr(), _type(_FLOAT, scores.dtype, "scores"), n, vocab, ld, tok.data_ptr(),
+        _type(_INDEX, tokens.dtype, "tokens"), tld, t.data_ptr(), _type(_FLOAT, teacher.dtype, "teacher"), eld, k)
+
+
+def distill(scores, tokens, teacher, temperature=1.0, stream=None):
+    """The loss [...] (float32) of scores [..., vocab] against a teacher's top logits, tokens and
+    teacher [..., k]: temperature^2 times the divergence of softmax(scores / temperature) from
+    softmax(teacher / temperature) over the entries.  Entries whose token is no column (padding,
+    -1) are none; a row without entries has loss 0."""
+    st = _stream(stream, scores, (tokens, teacher))
+    if st is None:
+        with _on(stream, scores):
+            return distill(scores, tokens, teacher, temperature)
+    held, sizes, args = _distilled(scores, tokens, teacher)
+    lib = _lib or _load()
+    ws = _workspace(lib.sp_distill_workspace, scores.device, *sizes, 0)
+    loss = torch.empty(scores.shape[:-1], dtype=torch.float32, device=scores.device)
+    _check(lib.sp_distill(*args, temperature, loss.data_ptr(), *((0, 0) if ws is None else (ws.data_ptr(), ws.shape[0])), st))
+    return loss
+
+
+def distill_grad(scores, tokens, teacher, weight=1.0, temperature=1.0, dtype=None, out=None, stream=None):
+    """distill's loss, and the gradient of the sum of weight * loss to the scores, in one pass.
+
+    weight: a number, or float32 of the loss's shape (what the loss's gradient is in the sum that is
+    trained, as 1 / rows).  dtype: the gradient's (default: the scores').  out may be scores."""
+    per_row = isinstance(weight, torch.Tensor)
+    st = _stream(stream, scores, (tokens, teacher, weight if per_row else None, out))
+    if st is None:
+        with _on(stream, scores):
+            return distill_grad(scores, tokens, teacher, weight, temperature, dtype, out)
+    held, sizes, args = _distilled(scores, tokens, teacher)
+    w = None
+    if per_row:
+        if weight.dtype != torch.float32 or weight.shape != scores.shape[:-1]:
+            raise _bad(f"weight {tuple(weight.shape)} {weight.dtype}, scores {tuple(scores.shape)}")
+        w = _flat(weight)
+    if dtype is None:
+        dtype = scores.dtype if out is None else out.dtype
+    lib = _lib or _load()
+    ws = _workspace(lib.sp_distill_workspace, scores.device, *sizes, 1)
+    loss = torch.empty(scores.shape[:-1], dtype=torch.float32, device=scores.device)
+    grad, to, old = _output(out, scores.shape, dtype, scores.device)
+    _check(lib.sp_distill_grad(
+        *args, temperature, 1.0 if per_row else weight, 0 if w is None else w.data_ptr(), loss.data_ptr(), to,
+        _type(_FLOAT, dtype, "out"), old, *((0, 0) if ws is None else (ws.data_ptr(), ws.shape[0])), st))
+    _changed(out)
+    return loss, grad

@@ -1,0 +1,225 @@
+"""Rows in 4 bits against plain implementations in 64 bits: codes, scales and values exactly, products
+within what k additions in fp32 and the output's rounding may be off."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+from paper_2205_04702_amd import scratchpipe as sp  # noqa: E402
+from paper_2205_04702_amd import tokens as tk  # noqa: E402
+from tests import scores_reference as ref  # noqa: E402
+from tests.rows_reference import TINY, UNIT  # noqa: E402
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def values(n, dim, seed, dtype):
+    """Values of all sizes that the type holds, many of them on the borders between codes."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, dim), generator=g)
+    borders = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 0.0])
+    at = borders[torch.randint(10, (n, dim), generator=g)] * (1 - 2 * torch.randint(2, (n, dim), generator=g))
+    x = torch.where(torch.rand((n, dim), generator=g) < 0.5, at, x)
+    low, high = (-20, 12) if dtype == F16 else (-140, 124)
+    by = torch.randint(low, high, (n, (dim + 31) // 32), generator=g).double().repeat_interleave(32, 1)[:, :dim]
+    return (x.double() * 2.0 ** by).float().to(dtype)
+
+
+def some_rows(n, k, seed, low=-4, high=5):
+    """Any codes, scales around 1, in the layout of empty_cache4: tensors on the GPU."""
+    g = torch.Generator().manual_seed(seed)
+    q, s = tk.empty_cache4(n, k)
+    code = torch.randint(16, (n, q.shape[1] * 2), generator=g).to(torch.uint8)
+    code[:, k:] = 0
+    q.copy_(code[:, 0::2] | code[:, 1::2] << 4)
+    s.copy_(torch.randint(127 + low, 127 + high, s.shape, generator=g).to(torch.uint8))
+    return q, s
+
+
+@pytest.mark.parametrize("n,dim,dtype", [(1, 1, F32), (3, 7, BF16), (2, 8, F16), (5, 31, F32), (4, 32, BF16), (9, 33, F16),
+                                         (130, 64, BF16), (70, 1001, F32), (33, 1024, F16), (3, 5000, BF16), (17, 2040, BF16)])
+def test_quantize_and_read(n, dim, dtype):
+    x = values(n, dim, dim, dtype)
+    q, s = tk.quantize4(x.cuda())
+    want_q, want_s = ref.quantize4(x)
+    assert torch.equal(s.cpu(), want_s)
+    assert torch.equal(q.cpu(), want_q)
+    back = tk.cache_read4(q, s, torch.arange(n, device="cuda"), dim, F32)
+    assert torch.equal(back.cpu().double(), ref.values4(want_q, want_s)[:, :dim])
+    whole = tk.cache_read4(q, s, torch.arange(n, device="cuda"), dtype=F32)
+    assert whole.shape == (n, (dim + 31) // 32 * 32) and not whole[:, dim:].any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_infinities_and_nan_stay_in_their_block(dtype):
+    x = torch.ones((4, 100), dtype=dtype)
+    x[0, 3], x[1, 40], x[2, 99] = math.inf, math.nan, -math.inf
+    q, s = tk.quantize4(x.cuda())
+    assert torch.equal(s.cpu(), ref.quantize4(x)[1]) and torch.equal(q.cpu(), ref.quantize4(x)[0])
+    back = tk.cache_read4(q, s, torch.arange(4, device="cuda"), 100, dtype).cpu()
+    bad = torch.zeros((4, 100), dtype=torch.bool)
+    bad[0, :32] = bad[1, 32:64] = bad[2, 96:] = True
+    assert torch.equal(torch.isnan(back), bad) and (back[~bad] == 1).all()
+    # a factor with such a block gives NaN in its rows of the product alone
+    w, ws = tk.quantize4(torch.ones((5, 100), dtype=dtype, device="cuda"))
+    assert torch.isnan(tk.product4(q, s, w, ws)).cpu().tolist() == [[True] * 5] * 3 + [[False] * 5]
+    assert torch.isnan(tk.product4(w, ws, q, s)).cpu().tolist() == [[True] * 3 + [False]] * 5
+
+
+@pytest.mark.parametrize("index", [torch.int32, torch.int64])
+@pytest.mark.parametrize("dim,dtype", [(64, BF16), (45, F32), (1000, F16)])
+def test_slots(dim, dtype, index):
+    """Writes into slots and reads of them; slots outside the cache; the rest left as it was."""
+    slots, n = 50, 21
+    q, s = some_rows(slots, dim, 3)
+    was_q, was_s = q.cpu(), s.cpu()
+    x = values(n, dim, 4, dtype)
+    to = torch.randperm(slots, generator=torch.Generator().manual_seed(5))[:n]
+    to[4], to[9], to[13] = -1, slots, 2 ** 31 - 1
+    tk.cache_write4(q, s, x.cuda(), to.to(index).cuda())
+    want_q, want_s = was_q.clone(), was_s.clone()
+    ok = (to >= 0) & (to < slots)
+    new_q, new_s = ref.quantize4(x)
+    want_q[to[ok]], want_s[to[ok]] = new_q[ok], new_s[ok]
+    assert torch.equal(q.cpu(), want_q) and torch.equal(s.cpu(), want_s)
+    at = torch.tensor([[0, -1, 7], [slots - 1, slots, 7]])
+    out = torch.full((2, 3, dim + 2), 9.0, device="cuda")[:, :, 1:1 + dim]
+    got = tk.cache_read4(q, s, at.to(index).cuda(), dim, F32, out=out)
+    want = ref.values4(want_q, want_s)[at.clamp(0, slots - 1)][..., :dim]
+    want[0, 1] = want[1, 1] = 0
+    assert torch.equal(got.cpu().double(), want)
+
+
+def test_strides_and_several_dimensions():
+    """Caches, rows and outputs with strides and odd starts; rows of heads."""
+    base_q = torch.full((12, 100), 7, dtype=torch.uint8, device="cuda")
+    base_s = torch.full((12, 9), 7, dtype=torch.uint8, device="cuda")
+    q, s = base_q[1:11, 3:67], base_s[1:11, 2:6]
+    x = values(10, 301, 6, BF16)[:, 1:127]
+    tk.cache_write4(q, s, x.cuda().view(10, 2, 63), torch.arange(10, device="cuda"))
+    want_q, want_s = ref.quantize4(x)
+    assert torch.equal(q.cpu(), want_q) and torch.equal(s.cpu(), want_s)
+    assert (base_q[0] == 7).all() and (base_q[:, :3] == 7).all() and (base_q[:, 67:] == 7).all()
+    assert (base_s[:, :2] == 7).all() and (base_s[:, 6:] == 7).all() and (base_s[11] == 7).all()
+    assert torch.equal(tk.cache_read4(q, s, torch.arange(10, device="cuda"), 126, F32).cpu().double(),
+                       ref.values4(want_q, want_s)[:, :126])
+    w, ws = some_rows(6, 128, 7)
+    want, off = ref.product4(want_q, want_s, w.cpu(), ws.cpu())
+    got = tk.product4(q, s, w, ws, F32).cpu().double()  # copied first: they start anywhere
+    assert ((got - want).abs() <= off + want.abs() * UNIT[F32]).all()
+
+
+def test_many_rows():
+    """Enough octets for the form with four per thread, in random slots."""
+    n, dim, slots = 9000, 1000, 12_000
+    x = values(n, dim, 8, BF16)
+    q, s = tk.empty_cache4(slots, dim)
+    to = torch.randperm(slots, generator=torch.Generator().manual_seed(9))[:n]
+    tk.cache_write4(q, s, x.cuda(), to.cuda())
+    want_q, want_s = ref.quantize4(x)
+    assert torch.equal(q.cpu()[to], want_q) and torch.equal(s.cpu()[to], want_s)
+    got = tk.cache_read4(q, s, to.cuda(), dim, F32)
+    assert torch.equal(got.cpu().double(), ref.values4(want_q, want_s)[:, :dim])
+
+
+# ------------------------------------------------------------------ products
+
+SHAPES = [(1, 1, 1), (1, 300, 32), (2, 5, 33), (3, 70, 100), (31, 33, 129), (33, 64, 512), (64, 200, 513), (65, 65, 640),
+          (100, 129, 1000), (130, 257, 2049), (257, 513, 300), (5, 2000, 4100), (300, 260, 96), (16, 24, 16384)]
+
+
+def close4(got, x, xs, w, ws, dtype):
+    want, off = ref.product4(x.cpu(), xs.cpu(), w.cpu(), ws.cpu())
+    bad = (got.cpu().double() - want).abs() - off - (want.abs() + off) * UNIT[dtype] - TINY[dtype]
+    assert not torch.isnan(bad).any() and bad.max() <= 0, bad.max()
+
+
+@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_product(m, n, k, dtype):
+    (x, xs), (w, ws) = some_rows(m, k, 11, -8, -3), some_rows(n, k, 12, -3, 4)
+    close4(tk.product4(x, xs, w, ws, dtype), x, xs, w, ws, dtype)
+
+
+@pytest.mark.parametrize("k", [1, 31, 32, 33, 64, 95, 96, 97, 128, 129, 384, 385, 511, 512, 544, 1024, 1056, 2080])
+def test_product_lengths(k):
+    """Every number of blocks in the last step, of steps in the last group of scales.  What lies behind
+    the rows and behind their scales counts nothing, and may be NaN."""
+    m, n = 40, 70
+    (x, xs), (w, ws) = some_rows(m, k, 13), some_rows(n, k, 14)
+    close4(tk.product4(x, xs, w, ws, F32), x, xs, w, ws, F32)
+    blocks = xs.shape[1]
+    for t in (xs, ws):
+        whole = torch.as_strided(t, (t.shape[0], t.stride(0)), t.stride())
+        whole[:, blocks:] = 255
+    for t in (x, w):
+        whole = torch.as_strided(t, (t.shape[0], t.stride(0)), t.stride())
+        whole[:, 16 * blocks:] = 0x77
+    close4(tk.product4(x, xs, w, ws, F32), x, xs, w, ws, F32)
+
+
+def test_product_of_the_smallest_and_largest_scales():
+    (x, xs), (w, ws) = some_rows(4, 64, 15), some_rows(40, 64, 16)
+    xs[0], xs[1], xs[2], xs[3] = 0, 1, 254, 127
+    ws.fill_(127)
+    ws[7] = 254
+    ws[9] = 0
+    want, off = ref.product4(x.cpu(), xs.cpu(), w.cpu(), ws.cpu())
+    got = tk.product4(x, xs, w, ws, F32).cpu().double()
+    # Where the terms' magnitudes add up to less than 2^128 no partial sum passes fp32's largest
+    # number; where they do not, one may, and the sum is infinite or NaN though the whole would fit.
+    fits = off / (66 * 2 ** -23) < 2.0 ** 128
+    assert ((got - want).abs() <= off + 2.0 ** -149)[fits].all() and (fits.sum(1) >= 30).tolist() == [True, True, False, True]
+    assert not torch.isfinite(got[want.abs() >= 2.0 ** 128]).any()
+
+
+def test_product_into_rows_of_a_larger_output():
+    (x, xs), (w, ws) = some_rows(37, 96, 17), some_rows(50, 96, 18)
+    buf = torch.full((39, 61), 5.0, dtype=BF16, device="cuda")
+    got = tk.product4(x, xs, w, ws, out=buf[1:38, 4:54], dtype=BF16)
+    close4(got, x, xs, w, ws, BF16)
+    buf[1:38, 4:54] = 5.0
+    assert (buf == 5.0).all()
+
+
+def test_product_of_rows_and_parts_of_rows():
+    """Slices of rows and of columns of a cache, one row, none."""
+    (x, xs), (w, ws) = some_rows(9, 256, 19), some_rows(80, 256, 20)
+    close4(tk.product4(x[2:7], xs[2:7], w[::2], ws[::2], F32), x[2:7], xs[2:7], w[::2], ws[::2], F32)
+    part = x[:, 16:48], xs[:, 1:3], w[:, 16:48], ws[:, 1:3]  # scales that start anywhere: copied
+    close4(tk.product4(*part, F32), *part, F32)
+    close4(tk.product4(x[3:4], xs[3:4], w[5:6], ws[5:6], F32), x[3:4], xs[3:4], w[5:6], ws[5:6], F32)
+    assert tk.product4(x[:0], xs[:0], w, ws).shape == (0, 80)
+
+
+def test_the_same_bits_again():
+    (x, xs), (w, ws) = some_rows(64, 8192, 21), some_rows(300, 8192, 22)
+    first = tk.product4(x, xs, w, ws, F32)
+    for _ in range(3):
+        assert torch.equal(tk.product4(x, xs, w, ws, F32), first)
+
+
+def test_refusals():
+    q, s = tk.empty_cache4(4, 64)
+    slots = torch.arange(4, device="cuda")
+    for call in (lambda: tk.cache_write4(q, s, torch.zeros((4, 65), device="cuda"), slots),
+                 lambda: tk.cache_write4(q, s, torch.zeros((3, 64), device="cuda"), slots),
+                 lambda: tk.cache_read4(q, s, slots, 97),
+                 lambda: tk.cache_read4(q, s, slots.float()),
+                 lambda: tk.cache_read4(q.to(torch.int8), s, slots),
+                 lambda: tk.cache_read4(q[:, :16], s, slots),
+                 lambda: tk.product4(q, s, q[:, :16], s[:, :1]),
+                 lambda: tk.product4(q, s[:3], q, s),
+                 lambda: tk.product4(q, s, q, s, dtype=torch.float64),
+                 lambda: tk.quantize4(torch.zeros((4, 0), device="cuda")),
+                 lambda: tk.quantize4(torch.zeros((4, 8), device="cuda", dtype=torch.float64))):
+        with pytest.raises(sp.SPError):
+            call()
