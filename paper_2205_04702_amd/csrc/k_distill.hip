@@ -13,13 +13,18 @@ namespace sp {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NONE = -__builtin_inff();
+constexpr int64_t CUS = 256;
 
 // A softmax's largest value and the sum of exp2((value - largest) * c), of a part of the values.
-// c is log2(e) / T: differences first, so that near the largest nothing is lost to c's rounding.
+// c is log2(e) / T: differences first, so that nothing is lost to c's rounding near the largest, and
+// scores of any size keep their order.  Exponentials below the smallest normal number are 0.
 struct Soft {
     float top, sum;
 };
-__device__ __forceinline__ float part_of(float v, float top, float c) { return exp2f((v - top) * c); }
+__device__ __forceinline__ float part_of(float v, float top, float c)
+{
+    return __builtin_amdgcn_exp2f((v - top) * c);
+}
 __device__ __forceinline__ void join(Soft &s, Soft o, float c)
 {
     const float top = fmaxf(s.top, o.top);
@@ -31,165 +36,371 @@ __device__ __forceinline__ void join(Soft &s, Soft o, float c)
     }
 }
 
-// The same over the block, in all of its threads.  `lds` holds NT / WAVE entries; two barriers.
-template <int NT>
-__device__ __forceinline__ Soft block_soft(Soft s, Soft *lds, float c)
+// ---------------------------------------------------------------- units
+//
+// A row is worked on in units of 16 bytes, at any address, and the columns behind its last whole unit
+// one by one.  Units are loaded and stored through the row's buffer descriptor, whose bounds the
+// hardware checks: past the last unit a load gives zeros and a store does nothing, with no branch
+// around either, so that the waits for a thread's loads can be counted (across branches they became
+// waits for everything in flight, and loads and stores took turns).
+typedef uint32_t unit __attribute__((ext_vector_type(4)));
+
+template <typename T>
+constexpr int COLS = 16 / (int)sizeof(T);
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *row, uint32_t bytes)
 {
-#pragma unroll
-    for (int o = WAVE / 2; o > 0; o >>= 1) {
-        const Soft other{__shfl_xor(s.top, o, WAVE), __shfl_xor(s.sum, o, WAVE)};
-        join(s, other, c);
-    }
-    if (lane_id() == 0) lds[wave_id()] = s;
-    __syncthreads();
-    s = lds[0];
-#pragma unroll
-    for (int w = 1; w < NT / WAVE; ++w) join(s, lds[w], c);
-    __syncthreads();
-    return s;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(row), 0, bytes, 0x00027000);
 }
-template <int NT>
-__device__ __forceinline__ float block_total(float v, float *lds)
+template <bool STREAM>
+__device__ __forceinline__ unit load_unit(__amdgpu_buffer_rsrc_t row, int32_t u)
 {
-    v = wave_sum(v);
-    if (lane_id() == 0) lds[wave_id()] = v;
-    __syncthreads();
-    v = lds[0];
+    return __builtin_amdgcn_raw_buffer_load_b128(row, (uint32_t)u * 16, 0, STREAM ? 2 : 0);
+}
+template <typename T>
+__device__ __forceinline__ float column(const unit &x, int k)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(x[k]);
+    const uint16_t h = (uint16_t)(x[k / 2] >> (k % 2 * 16));
+    T v;
+    __builtin_memcpy(&v, &h, sizeof(T) < 4 ? sizeof v : 0);
+    return to_float(v);
+}
+template <typename T>
+__device__ __forceinline__ unit all_of(float x)
+{
+    const T v = from_float<T>(x);
+    uint32_t w = 0;
+    __builtin_memcpy(&w, &v, sizeof v);
+    if (sizeof(T) == 2) w |= w << 16;
+    return unit{w, w, w, w};
+}
+// Columns of a unit of the scores, as the output's type.
+template <bool STREAM, typename TO, int C>
+__device__ __forceinline__ void store_unit(__amdgpu_buffer_rsrc_t row, int32_t u, const float (&v)[C])
+{
+    Pack<TO, C> p;
 #pragma unroll
-    for (int w = 1; w < NT / WAVE; ++w) v += lds[w];
-    __syncthreads();
-    return v;
+    for (int k = 0; k < C; ++k) p.v[k] = from_float<TO>(v[k]);
+    constexpr int BYTES = (int)sizeof p, AUX = STREAM ? 2 : 0;
+    if constexpr (BYTES == 8) {
+        uint32_t w __attribute__((ext_vector_type(2)));
+        __builtin_memcpy(&w, &p, 8);
+        __builtin_amdgcn_raw_buffer_store_b64(w, row, (uint32_t)u * 8, 0, AUX);
+    } else {
+#pragma unroll
+        for (int i = 0; i < BYTES / 16; ++i) {
+            unit w;
+            __builtin_memcpy(&w, (const char *)&p + 16 * i, 16);
+            __builtin_amdgcn_raw_buffer_store_b128(w, row, (uint32_t)(u * BYTES + 16 * i), 0, AUX);
+        }
+    }
 }
 
-// An octet into a part of the softmax: one rescaling for its eight columns.
-template <typename T>
-__device__ __forceinline__ void add_oct(Soft &s, const float (&v)[OCT], int valid, float c)
+// N units of a thread into a part of the softmax: one rescaling for all of their columns.
+template <typename T, int N>
+__device__ __forceinline__ void add_units(Soft &s, const unit *x, float c)
 {
     float top = s.top;
 #pragma unroll
-    for (int k = 0; k < OCT; ++k) top = fmaxf(top, k < valid ? v[k] : NONE);
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int k = 0; k < COLS<T>; ++k) top = fmaxf(top, column<T>(x[i], k));
     const float base = top > NONE ? top : 0.f;
     float sum = s.top > NONE ? s.sum * part_of(s.top, base, c) : s.sum;
 #pragma unroll
-    for (int k = 0; k < OCT; ++k) sum += k < valid ? part_of(v[k], base, c) : 0.f;
+    for (int i = 0; i < N; ++i) {
+        float part = 0.f;
+#pragma unroll
+        for (int k = 0; k < COLS<T>; ++k) part += part_of(column<T>(x[i], k), base, c);
+        sum += part;
+    }
     s = Soft{top, sum};
 }
 
-// ---------------------------------------------------------------- the teacher's entries
+// ---------------------------------------------------------------- tokens that are listed twice
 //
-// Entries in LDS, a thread at a time for each NT-th.  Tokens that are listed more than once
-// are found with a hash of the tokens, in which each keeps the lowest entry that lists it.
-constexpr int MAX_K = 1024, SLOTS = 2 * MAX_K;
-struct Entries {
-    int32_t token[MAX_K];  // -1: none
-    float p[MAX_K], score[MAX_K];
-    int32_t key[SLOTS], lowest[SLOTS];
-    int32_t repeated;
-};
+// A hash of a row's tokens, in which each keeps the lowest entry that lists it.
 constexpr int32_t FREE = -1;
 
-__device__ __forceinline__ int slot_of(const Entries &e, int32_t token, int mask)
+template <int K>
+struct Hash {
+    int32_t key[2 * K], lowest[2 * K];
+    int32_t repeated;
+};
+__device__ __forceinline__ int hash_of(int32_t token, int mask) { return (int)((uint32_t)token * 0x9E3779B1u >> 16) & mask; }
+__device__ __forceinline__ int hash_mask(int k)  // at most half of the slots are taken
 {
-    int h = (int)((uint32_t)token * 0x9E3779B1u >> 16) & mask;
-    while (e.key[h] != token) h = (h + 1) & mask;
-    return h;
+    int mask = 1;
+    while (mask < 2 * k) mask *= 2;
+    return mask - 1;
+}
+template <int K>
+__device__ __forceinline__ void clear(Hash<K> &h, int mask)
+{
+    for (int i = (int)threadIdx.x; i <= mask; i += (int)blockDim.x) h.key[i] = FREE, h.lowest[i] = K;
+    if (threadIdx.x == 0) h.repeated = 0;
+}
+template <int K>
+__device__ __forceinline__ void note(Hash<K> &h, int mask, int32_t token, int j)
+{
+    int at = hash_of(token, mask);
+    for (;;) {
+        const int32_t old = atomicCAS(&h.key[at], FREE, token);
+        if (old == token) h.repeated = 1;
+        if (old == FREE || old == token) break;
+        at = (at + 1) & mask;
+    }
+    atomicMin(&h.lowest[at], j);
+}
+template <int K>
+__device__ __forceinline__ bool is_lowest(const Hash<K> &h, int mask, int32_t token, int j)
+{
+    int at = hash_of(token, mask);
+    while (h.key[at] != token) at = (at + 1) & mask;
+    return h.lowest[at] == j;
 }
 
-// One block per row, which is read once for the sums and, for the gradient, once more.
-template <typename T, typename TO, int NT, bool GRAD>
-__global__ void __launch_bounds__(NT) k_distill(DistillArgs a)
+// ---------------------------------------------------------------- entries
+//
+// Thread j has entry j of the teacher (k <= NT): its token (-1: none), logit and score.
+struct Entry {
+    int32_t token;
+    float logit, score;
+};
+// An entry (and the row's weight) as loaded: taken apart only when it is needed, so that nothing waits for it.
+struct RawEntry {
+    uint32_t low, high, logit, score;
+    float weight;
+};
+__device__ __forceinline__ void load_entry(const DistillArgs &a, int64_t row, RawEntry &r)
 {
-    __shared__ Soft soft[NT / WAVE];
-    __shared__ float total[NT / WAVE];
-    __shared__ Entries e;
-    const int64_t row = blockIdx.x;
-    const int t = (int)threadIdx.x;
-    const float c = LOG2E / a.temperature;
-    const T *scores = (const T *)a.scores + row * a.ld;
-    const Cols cols = cols_of(a.vocab);
-    const int32_t octs = (a.vocab + OCT - 1) / OCT;
-    TO *grad = GRAD ? (TO *)a.grad + row * a.grad_ld : nullptr;
-
-    int mask = 1;
-    while (mask < 2 * a.k) mask *= 2;
-    mask -= 1;
-    if (GRAD) {
-        for (int i = t; i <= mask; i += NT) e.key[i] = FREE, e.lowest[i] = MAX_K;
-        if (t == 0) e.repeated = 0;
+    r.weight = a.weights ? a.weights[row] : a.weight;
+    if ((int)threadIdx.x >= a.k) return;
+    const int64_t at = row * a.tokens_ld + threadIdx.x, from = row * a.teacher_ld + threadIdx.x;
+    if (a.token_type == 3) {
+        r.low = ((const uint32_t *)a.tokens)[at];
+    } else {
+        r.low = ((const uint32_t *)a.tokens)[2 * at];
+        r.high = ((const uint32_t *)a.tokens)[2 * at + 1];
     }
-    Soft teacher{NONE, 0.f};
-    for (int j = t; j < a.k; j += NT) {
-        const int64_t token = index_at(a.tokens, a.token_type, row * a.tokens_ld + j);
-        const bool live = token >= 0 && token < a.vocab;
-        const float v = live ? float_at(a.teacher, a.teacher_type, row * a.teacher_ld + j) : NONE;
-        e.token[j] = live ? (int32_t)token : -1;
-        e.p[j] = v;
-        e.score[j] = live ? to_float(scores[token]) : 0.f;
-        join(teacher, Soft{v, v > NONE ? 1.f : v != v ? v : 0.f}, c);
-    }
-    teacher = block_soft<NT>(teacher, soft, c);
-    if (teacher.sum == 0.f) {  // the same for all
-        if (t == 0) a.loss[row] = 0.f;
-        if (GRAD) {
-            const float zeros[OCT] = {};
-            for (int32_t o = t; o < octs; o += NT) put_row_oct(grad, o, a.vocab, false, zeros);
-        }
-        return;
-    }
-
-    Soft s{NONE, 0.f};
-    for (int32_t o = t; o < octs; o += NT) {
-        float v[OCT];
-        load_oct<false, false>(scores, o, cols, v);
-        add_oct<T>(s, v, oct_valid(a.vocab, o), c);
-    }
-    s = block_soft<NT>(s, soft, c);
-    const float log_sum = log2f(s.sum) * LN2, log_mass = log2f(teacher.sum) * LN2;
-    const float per_t = 1.f / a.temperature, mass = 1.f / teacher.sum;
-
-    float loss = 0.f;
-    for (int j = t; j < a.k; j += NT) {
-        const float v = e.p[j], p = part_of(v, teacher.top, c) * mass;
-        const float log_p = (v - teacher.top) * per_t - log_mass;
-        const float log_q = (e.score[j] - s.top) * per_t - log_sum;
-        if (e.token[j] >= 0 && !(p == 0.f)) loss += p * (log_p - (s.sum == 0.f ? NONE : log_q));
-        e.p[j] = e.token[j] >= 0 ? p : 0.f;
-        if (GRAD && e.token[j] >= 0) {
-            int h = (int)((uint32_t)e.token[j] * 0x9E3779B1u >> 16) & mask;
-            for (;;) {  // (at most half of the slots are taken)
-                const int32_t old = atomicCAS(&e.key[h], FREE, e.token[j]);
-                if (old == FREE) break;
-                if (old == e.token[j]) {
-                    e.repeated = 1;
-                    break;
-                }
-                h = (h + 1) & mask;
-            }
-            atomicMin(&e.lowest[h], j);
-        }
-    }
-    loss = block_total<NT>(loss, total);
-    if (t == 0) a.loss[row] = loss * a.temperature * a.temperature;
-    if (!GRAD) return;
-
-    const float g = (a.weights ? a.weights[row] : a.weight) * a.temperature;
-    const float base = s.top > NONE ? s.top : 0.f, part = s.sum == 0.f ? 0.f : 1.f / s.sum;
-    for (int32_t o = t; o < octs; o += NT) {
-        float v[OCT];
-        load_oct<false, false>(scores, o, cols, v);
+    r.logit = a.teacher_type == 0 ? ((const uint32_t *)a.teacher)[from] : ((const uint16_t *)a.teacher)[from];
+}
+__device__ __forceinline__ Entry entry_of(const DistillArgs &a, const RawEntry &r)
+{
+    Entry e{-1, NONE, 0.f};
+    if ((int)threadIdx.x >= a.k || r.low >= (uint32_t)a.vocab || (a.token_type != 3 && r.high != 0)) return e;
+    e.token = (int32_t)r.low;
+    const uint16_t h = (uint16_t)r.logit;
+    __bf16 b;
+    _Float16 f;
+    __builtin_memcpy(&b, &h, 2);
+    __builtin_memcpy(&f, &h, 2);
+    e.logit = a.teacher_type == 0 ? __uint_as_float(r.logit) : a.teacher_type == 1 ? to_float(b) : to_float(f);
+    return e;
+}
+template <typename T>
+__device__ __forceinline__ void load_score(const Entry &e, const T *scores, RawEntry &r)
+{
+    if (e.token < 0) return;
+    if (sizeof(T) == 4) r.score = ((const uint32_t *)scores)[e.token];
+    else r.score = ((const uint16_t *)scores)[e.token];
+}
+template <typename T>
+__device__ __forceinline__ float score_of(const Entry &e, const RawEntry &r)
+{
+    return e.token < 0 ? 0.f : column<T>(unit{r.score, 0, 0, 0}, 0);
+}
+__device__ __forceinline__ Soft soft_of(const Entry &e)
+{
+    return Soft{e.logit, e.logit > NONE ? 1.f : e.logit != e.logit ? e.logit : 0.f};
+}
+// An entry's p, and its part of the loss without T^2.
+__device__ __forceinline__ float mass_of(const Entry &e, Soft teacher, float c)
+{
+    return e.token >= 0 ? part_of(e.logit, teacher.top, c) / teacher.sum : 0.f;
+}
+__device__ __forceinline__ float loss_of(const Entry &e, float p, Soft teacher, Soft s, float temperature)
+{
+    const float log_p = (e.logit - teacher.top) / temperature - __builtin_amdgcn_logf(teacher.sum) * LN2;
+    const float log_q = s.sum == 0.f ? NONE : (e.score - s.top) / temperature - __builtin_amdgcn_logf(s.sum) * LN2;
+    return p == 0.f ? 0.f : p * (log_p - log_q);
+}
+__device__ __forceinline__ Soft wave_soft(Soft s, float c)
+{
 #pragma unroll
-        for (int k = 0; k < OCT; ++k) v[k] = part_of(v[k], base, c) * part * g;
-        put_row_oct(grad, o, a.vocab, false, v);
-    }
+    for (int o = WAVE / 2; o > 0; o >>= 1) join(s, Soft{__shfl_xor(s.top, o, WAVE), __shfl_xor(s.sum, o, WAVE)}, c);
+    return s;
+}
+
+// ---------------------------------------------------------------- a block for a row
+//
+// A row is read once: HELD units a thread stay in registers as they were loaded, between the sums and
+// the gradient; what a longer row has beyond is read again.  A block goes from row to row, and loads
+// the next one's units into the registers that the gradient's stores leave, so that loads, stores and
+// exponentials of a block overlap although most often one block fills a CU.  Two barriers a row: after
+// the sums, and between the gradient and its corrections in the teacher's columns, which go over what
+// was stored.
+template <typename T, typename TO, int NT, int HELD, bool GRAD, bool STREAM>
+__global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(DistillArgs a)
+{
+    constexpr int N = 4, C = COLS<T>, NW = NT / WAVE;  // N units are added at once
+    static_assert(HELD % N == 0, "whole steps");
+    __shared__ Soft sums[NW], masses[NW];
+    __shared__ float losses[NW];
+    __shared__ int32_t alive[2][NW];
+    __shared__ Hash<NT> hash[2];
+    __shared__ int32_t tokens[NT];
+    __shared__ float ps[NT];
+    int t = (int)threadIdx.x;
+    const int wave = wave_id(), entry_waves = (a.k + WAVE - 1) / WAVE, mask = hash_mask(a.k);
+    const float c = LOG2E / a.temperature;
+    const int32_t units = a.vocab / C, rest = a.vocab - units * C;
+    const auto scores_of = [&](int64_t row) { return (const T *)a.scores + row * a.ld; };
+    // Whether any entry of a row counts, from what each wave found; a barrier lies between.
+    const auto note_alive = [&](int turn, const Entry &e) {
+        const bool on = __any(!(e.logit == NONE));
+        if (lane_id() == 0) alive[turn][wave] = on;
+    };
+    const auto is_alive = [&](int turn) {
+        int32_t on = 0;
+        for (int w = 0; w < entry_waves; ++w) on |= alive[turn][w];
+        return on != 0;
+    };
+
+    unit r[HELD];
+    T last = from_float<T>(0.f);  // a column behind the last unit
+    int64_t row = blockIdx.x;
+    RawEntry raw{};
+    load_entry(a, row, raw);
+    Entry e = entry_of(a, raw);
+    note_alive(1, e);
+    if (GRAD) clear(hash[0], mask);
     __syncthreads();
-    // The teacher's columns again, over what was stored: the lowest entry of each token.
-    for (int j = t; j < a.k; j += NT) {
-        const int32_t token = e.token[j];
-        if (token < 0 || e.lowest[slot_of(e, token, mask)] != j) continue;
-        float p = e.p[j];
-        if (e.repeated)
-            for (int i = j + 1; i < a.k; ++i) p += e.token[i] == token ? e.p[i] : 0.f;
-        grad[token] = from_float<TO>((part_of(e.score[j], base, c) * part - p) * g);
+    bool on = is_alive(1);
+    load_score(e, scores_of(row), raw);
+    if (t < rest) last = scores_of(row)[units * C + t];
+    {
+        const __amdgpu_buffer_rsrc_t from = buffer(scores_of(row), on ? units * 16 : 0);
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) r[i] = load_unit<STREAM>(from, t + i * NT);
+    }
+    for (int turn = 0;; turn ^= 1) {
+        // (else every unit's place is worked out before the loop and kept)
+        asm volatile("" : "+v"(t));
+        const T *scores = scores_of(row);
+        const bool more = row + gridDim.x < a.n;
+        const int64_t next = more ? row + gridDim.x : row;
+        RawEntry raw_next{};
+        load_entry(a, next, raw_next);
+        Soft s{NONE, 0.f};
+        if (on) {
+#pragma unroll
+            for (int i = 0; i < HELD; i += N)
+                if (i * NT < units) {
+                    if ((i + N) * NT > units) {
+#pragma unroll
+                        for (int k = i; k < i + N; ++k)
+                            if (t + k * NT >= units) r[k] = all_of<T>(NONE);
+                    }
+                    add_units<T, N>(s, r + i, c);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            const __amdgpu_buffer_rsrc_t from = buffer(scores, units * 16);
+            for (int32_t u = HELD * NT + t; u < units; u += N * NT) {
+                unit x[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[k] = load_unit<false>(from, u + k * NT);
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (u + k * NT >= units) x[k] = all_of<T>(NONE);
+                add_units<T, N>(s, x, c);
+            }
+            if (t < rest) {
+                const float v = to_float(last);
+                join(s, Soft{v, v > NONE ? 1.f : v != v ? v : 0.f}, c);
+            }
+            s = wave_soft(s, c);
+            if (lane_id() == 0) sums[wave] = s;
+            if (wave < entry_waves) {
+                const Soft m = wave_soft(soft_of(e), c);
+                if (lane_id() == 0) masses[wave] = m;
+            }
+        }
+        Entry f = entry_of(a, raw_next);
+        note_alive(turn, f);
+        __syncthreads();
+        const bool next_on = more && is_alive(turn);
+        const __amdgpu_buffer_rsrc_t from = buffer(scores_of(next), next_on ? units * 16 : 0);
+        const T own = last;
+        if (next_on) {
+            load_score(f, scores_of(next), raw_next);
+            if (t < rest) last = scores_of(next)[units * C + t];
+        }
+        Soft m{NONE, 0.f};
+        float p = 0.f;
+        if (on) {
+            s = sums[0];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) join(s, sums[w], c);
+            for (int w = 0; w < entry_waves; ++w) join(m, masses[w], c);
+            if (wave < entry_waves) {
+                e.score = score_of<T>(e, raw);
+                p = mass_of(e, m, c);
+                const float loss = wave_sum(loss_of(e, p, m, s, a.temperature));
+                if (lane_id() == 0) losses[wave] = loss;
+                if (GRAD) {
+                    tokens[t] = e.token;
+                    ps[t] = p;
+                    if (e.token >= 0) note(hash[turn], mask, e.token, t);
+                }
+            }
+        }
+        if (GRAD) {
+            clear(hash[turn ^ 1], mask);
+            TO *grad = (TO *)a.grad + row * a.grad_ld;
+            const __amdgpu_buffer_rsrc_t to = buffer(grad, units * C * (int)sizeof(TO));
+            const float g = raw.weight * a.temperature;
+            const float base = s.top > NONE ? s.top : 0.f, part = !on || s.sum == 0.f ? 0.f : 1.f / s.sum, by = part * g;
+            const auto store = [&](unit x, int32_t u) {
+                float v[C];
+                // (converted again: else the sums' fp32 values are kept in registers till here)
+                asm("" : "+v"(x));
+#pragma unroll
+                for (int k = 0; k < C; ++k) v[k] = on ? part_of(column<T>(x, k), base, c) * by : 0.f;
+                store_unit<STREAM, TO>(to, u, v);
+            };
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                store(r[i], t + i * NT);
+                r[i] = load_unit<STREAM>(from, t + i * NT);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const __amdgpu_buffer_rsrc_t again = buffer(scores, on ? units * 16 : 0);
+            for (int32_t u = HELD * NT + t; u < units; u += NT) store(load_unit<STREAM>(again, u), u);
+            if (t < rest) grad[units * C + t] = from_float<TO>(on ? part_of(to_float(own), base, c) * by : 0.f);
+            __syncthreads();
+            if (on && e.token >= 0 && is_lowest(hash[turn], mask, e.token, t)) {
+                if (hash[turn].repeated)
+                    for (int i = t + 1; i < a.k; ++i) p += tokens[i] == e.token ? ps[i] : 0.f;
+                grad[e.token] = from_float<TO>((part_of(e.score, base, c) * part - p) * g);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) r[i] = load_unit<STREAM>(from, t + i * NT);
+            __syncthreads();
+        }
+        if (t == 0) {
+            float loss = 0.f;
+            if (on)
+                for (int w = 0; w < entry_waves; ++w) loss += losses[w];
+            a.loss[row] = loss * a.temperature * a.temperature;
+        }
+        if (!more) return;
+        row = next;
+        e = f;
+        raw = raw_next;
+        on = next_on;
     }
 }
 
@@ -201,20 +412,24 @@ hipError_t run_distill(const DistillArgs &given, hipStream_t s)
         return with_type(given.grad ? given.grad_type : 0, [&](auto to) {
             using T = decltype(ti);
             using TO = decltype(to);
-            for (int64_t i = 0; i < given.n; i += LAUNCH_BLOCKS) {
-                DistillArgs a = given;
-                a.n = given.n - i < LAUNCH_BLOCKS ? given.n - i : LAUNCH_BLOCKS;
-                a.scores = (const T *)given.scores + i * given.ld;
-                a.tokens = index_past(given.tokens, given.token_type, i * given.tokens_ld);
-                a.teacher = (const char *)given.teacher + i * given.teacher_ld * (given.teacher_type == 0 ? 4 : 2);
-                a.loss += i;
-                if (a.weights) a.weights += i;
-                if (a.grad) a.grad = (TO *)given.grad + i * given.grad_ld;
-                const hipError_t e = a.grad ? launch(k_distill<T, TO, BLOCK, true>, dim3((unsigned)a.n), dim3(BLOCK), s, a)
-                                            : launch(k_distill<T, float, BLOCK, false>, dim3((unsigned)a.n), dim3(BLOCK), s, a);
-                if (e != hipSuccess) return e;
-            }
-            return hipSuccess;
+            const int64_t units = given.vocab / COLS<T>;
+            const auto go = [&](auto kern, int nt, int waves) {
+                const int64_t blocks = waves ? CUS * waves * WAVE / nt : LAUNCH_BLOCKS / 2;
+                return launch(kern, dim3((unsigned)(given.n < blocks ? given.n : blocks)), dim3(nt), s, given);
+            };
+            const auto pick = [&](auto stream) {
+                constexpr bool S = decltype(stream)::value;
+                if (given.k <= 64 && units <= 64 * 4) return go(k_distill<T, TO, 64, 4, true, S>, 64, 20);
+                if (given.k <= 64 && units <= 64 * 16) return go(k_distill<T, TO, 64, 16, true, S>, 64, 16);
+                if (given.k <= 256 && units <= 256 * 4) return go(k_distill<T, TO, 256, 4, true, S>, 256, 20);
+                if (given.k <= 256 && units <= 256 * 16) return go(k_distill<T, TO, 256, 16, true, S>, 256, 16);
+                if (given.k <= 512 && units <= 512 * 16) return go(k_distill<T, TO, 512, 16, true, S>, 512, 16);
+                return go(k_distill<T, TO, 1024, 16, true, S>, 1024, 16);
+            };
+            if (!given.grad)
+                return given.k <= 256 ? go(k_distill<T, float, 256, 4, false, true>, 256, 0)
+                                      : go(k_distill<T, float, 1024, 4, false, true>, 1024, 0);
+            return whole_pieces((const TO *)given.grad, given.grad_ld) ? pick(std::true_type()) : pick(std::false_type());
         });
     });
 }

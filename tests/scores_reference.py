@@ -100,7 +100,8 @@ def distill(scores, tokens, teacher, weight, T):
     and c itself, off by 4 U of its size a at most, and the exponential by 3 U more: a term is within
     r(a) = U (4 a + 3) of itself.  A sum of them passes at most vocab / 64 + 100 additions and 60 joins,
     each of which scales by another exponential: the differences of its exponents add up to the largest
-    a, so all of them cost U (4 a + 4 * 60)."""
+    a, so all of them cost U (4 a + 4 * 60).  Exponentials below 2^-126 of the largest are 0: as many of
+    them as there are columns change a sum by less than U, and a column's gradient by w T 2^-126."""
     n, vocab = scores.shape
     loss = torch.zeros(n, dtype=torch.float64)
     grad = torch.zeros((n, vocab), dtype=torch.float64)
@@ -125,7 +126,7 @@ def distill(scores, tokens, teacher, weight, T):
         def softmax_off(z, terms):
             a = torch.where(torch.isfinite(z), (z.max() - z) / math.log(2), torch.zeros_like(z))
             reach = min(a.max().item(), 200.0)  # (terms past 2^-200 of the sum count nothing)
-            total = U32 * (4 * reach + 4 * 60 + terms / 64 + 100 + 4 * reach + 3)
+            total = U32 * (4 * reach + 4 * 60 + terms / 64 + 101 + 4 * reach + 3)
             return U32 * (4 * a + 3) + total + 3 * U32, total
 
         p_off, teacher_off = softmax_off(t, len(t))
@@ -141,5 +142,5 @@ def distill(scores, tokens, teacher, weight, T):
         mass_off = torch.zeros_like(z).index_add_(0, tok[live], (p * (p_off + (len(t) + 4) * U32))[live])
         w = abs(float(weight[i])) * T
         grad[i] *= float(weight[i]) * T
-        grad_off[i] = w * (q * q_off + mass_off + 6 * U32 * (q + mass))
+        grad_off[i] = w * (q * q_off + mass_off + 6 * U32 * (q + mass) + 2.0 ** -126)
     return loss, grad, loss_off + 1e-44, grad_off
