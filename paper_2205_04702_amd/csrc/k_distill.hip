@@ -13,7 +13,8 @@ namespace sp {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NONE = -__builtin_inff();
-constexpr int64_t CUS = 256;
+constexpr int64_t CUS = 256, FEW_ROWS = 64;
+constexpr int32_t LONG_ROW = 49152;
 
 // A softmax's largest value and the sum of exp2((value - largest) * c), of a part of the values.
 // c is log2(e) / T: differences first, so that nothing is lost to c's rounding near the largest, and
@@ -469,7 +470,157 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
     }
 }
 
-int64_t distill_workspace(int64_t, int32_t, int32_t, bool) { return 0; }
+// ---------------------------------------------------------------- few rows
+//
+// Rows too few to fill the card are cut into parts of whole units: sums of each part, then (a second
+// launch) each block joins its row's and goes on with its part.  The entries' scores are kept by the
+// first launch, for the second may store over them.
+struct Parts {
+    int32_t parts, columns;  // of a part, a multiple of 8
+    Soft *sums;              // [n][parts]
+    float *scores;           // [n][k]
+};
+// Parts so that there are two blocks a CU, of 4096 columns at least.  Whole rows and parts (us a call
+// with gradient, of which the host takes 11 and, for two launches, 15): 131072 columns in bf16 1 row 18.9
+// and 15.1, 64 rows 21.8 and 15.6, 128 rows 22.6 and 23.8; in fp32 64 rows 26.1 and 21.7, 128 rows 31.9
+// and 42.0; 50001 columns in bf16 16 rows 15.3 and 15.3, 64 rows 16.1 and 15.3.
+static Parts cut_rows(int64_t n, int32_t vocab, char *work)
+{
+    const int64_t most = (vocab + 4095) / 4096, want = n > 0 ? (2 * CUS + n - 1) / n : 1;
+    const int64_t parts = n <= FEW_ROWS && vocab >= LONG_ROW ? (want < most ? want : most) : 1;
+    const int32_t columns = (int32_t)(((vocab + parts - 1) / parts + 7) / 8 * 8);
+    return Parts{(vocab + columns - 1) / columns, columns, (Soft *)work, nullptr};
+}
+
+template <typename T>
+__global__ void __launch_bounds__(BLOCK) k_distill_part(DistillArgs a, Parts q)
+{
+    constexpr int N = 4, C = COLS<T>, NW = BLOCK / WAVE;
+    __shared__ Soft sums[NW];
+    const int64_t row = blockIdx.y;
+    const int part = (int)blockIdx.x, t = (int)threadIdx.x;
+    const float c = LOG2E / a.temperature;
+    const T *scores = (const T *)a.scores + row * a.ld;
+    const int32_t units = a.vocab / C, rest = a.vocab - units * C;
+    const int32_t first = part * (q.columns / C);
+    int32_t end = first + q.columns / C;
+    if (end > units) end = units;
+    const __amdgpu_buffer_rsrc_t from = buffer(scores, units * 16);
+    Soft s{NONE, 0.f};
+    for (int32_t u = first + t; u < end; u += N * BLOCK) {
+        unit x[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = load_unit<false>(from, u + k * BLOCK);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (u + k * BLOCK >= end) x[k] = all_of<T>(NONE);
+        add_units<T, N>(s, x, c);
+    }
+    if (part == q.parts - 1 && t < rest) {
+        const float v = to_float(scores[units * C + t]);
+        join(s, Soft{v, v > NONE ? 1.f : v != v ? v : 0.f}, c);
+    }
+    if (part == 0)
+        for (int j = t; j < a.k; j += BLOCK) {
+            const int64_t token = index_at(a.tokens, a.token_type, row * a.tokens_ld + j);
+            q.scores[row * a.k + j] = token >= 0 && token < a.vocab ? to_float(scores[token]) : 0.f;
+        }
+    s = wave_soft(s, c);
+    if (lane_id() == 0) sums[wave_id()] = s;
+    __syncthreads();
+    if (t == 0) {
+#pragma unroll
+        for (int w = 1; w < NW; ++w) join(s, sums[w], c);
+        q.sums[row * q.parts + part] = s;
+    }
+}
+
+template <typename T, typename TO, int NT, bool GRAD>
+__global__ void __launch_bounds__(NT) k_distill_rest(DistillArgs a, Parts q)
+{
+    constexpr int N = 4, C = COLS<T>, NW = NT / WAVE;
+    __shared__ Soft masses[NW];
+    __shared__ float losses[NW];
+    __shared__ Hash<NT> hash;
+    __shared__ int32_t tokens[NT];
+    __shared__ float ps[NT];
+    const int64_t row = blockIdx.y;
+    const int part = (int)blockIdx.x, t = (int)threadIdx.x, wave = wave_id();
+    const int entry_waves = (a.k + WAVE - 1) / WAVE, mask = hash_mask(a.k);
+    const float c = LOG2E / a.temperature;
+    const T *scores = (const T *)a.scores + row * a.ld;
+    const int32_t units = a.vocab / C, rest = a.vocab - units * C;
+    const int32_t first = part * (q.columns / C);
+    int32_t end = first + q.columns / C;
+    if (end > units) end = units;
+
+    RawEntry raw{};
+    load_entry(a, row, raw);
+    Soft s{NONE, 0.f};
+    for (int i = lane_id(); i < q.parts; i += WAVE) join(s, q.sums[row * q.parts + i], c);
+    s = wave_soft(s, c);
+    Entry e = entry_of(a, raw);
+    if (e.token >= 0) e.score = q.scores[row * a.k + t];
+    if (wave < entry_waves) {
+        const Soft m = wave_soft(soft_of(e), c);
+        if (lane_id() == 0) masses[wave] = m;
+    }
+    if (GRAD) clear(hash, mask);
+    __syncthreads();
+    Soft m{NONE, 0.f};
+    for (int w = 0; w < entry_waves; ++w) join(m, masses[w], c);
+    const bool on = !(m.sum == 0.f);
+    float p = 0.f;
+    if (on && wave < entry_waves) {
+        p = mass_of(e, m, c);
+        const float loss = wave_total(loss_of(e, p, m, s, a.temperature));
+        if (lane_id() == 0) losses[wave] = loss;
+        if (GRAD) {
+            tokens[t] = e.token;
+            ps[t] = p;
+            if (e.token >= 0) note(hash, mask, e.token, t);
+        }
+    }
+    if (GRAD) {
+        TO *grad = (TO *)a.grad + row * a.grad_ld;
+        const __amdgpu_buffer_rsrc_t from = buffer(scores, on ? end * 16 : 0), to = buffer(grad, end * C * (int)sizeof(TO));
+        const float g = raw.weight * a.temperature;
+        const float base = s.top > NONE ? s.top : 0.f, by = !on || s.sum == 0.f ? 0.f : g / s.sum;
+        for (int32_t u = first + t; u < end; u += N * NT) {
+            unit x[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = load_unit<false>(from, u + i * NT);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float v[C];
+#pragma unroll
+                for (int k = 0; k < C; ++k) v[k] = on ? part_of(column<T>(x[i], k), base, c) * by : 0.f;
+                store_unit<false, TO>(to, u + i * NT, v);
+            }
+        }
+        const bool own_rest = part == q.parts - 1;
+        if (own_rest && t < rest)
+            grad[units * C + t] = from_float<TO>(on ? part_of(to_float(scores[units * C + t]), base, c) * by : 0.f);
+        __syncthreads();  // the teacher's columns again, over what was stored
+        if (on && e.token >= 0 && ((e.token >= first * C && e.token < end * C) || (own_rest && e.token >= units * C)) &&
+            is_first(hash, mask, e.token, t))
+            grad[e.token] = from_float<TO>(part_of(e.score, base, c) * by - listed(hash, mask, e.token, tokens, ps) * g);
+    } else {
+        __syncthreads();
+    }
+    if (part == 0 && t == 0) {
+        float loss = 0.f;
+        if (on)
+            for (int w = 0; w < entry_waves; ++w) loss += losses[w];
+        a.loss[row] = loss * a.temperature * a.temperature;
+    }
+}
+
+int64_t distill_workspace(int64_t n, int32_t vocab, int32_t k, bool)
+{
+    const Parts q = cut_rows(n, vocab, nullptr);
+    return q.parts > 1 ? n * (q.parts * (int64_t)sizeof(Soft) + k * (int64_t)sizeof(float)) : 0;
+}
 
 hipError_t run_distill(const DistillArgs &given, hipStream_t s)
 {
@@ -482,6 +633,18 @@ hipError_t run_distill(const DistillArgs &given, hipStream_t s)
                 const int64_t blocks = waves ? CUS * waves * WAVE / nt : LAUNCH_BLOCKS / 2;
                 return launch(kern, dim3((unsigned)(given.n < blocks ? given.n : blocks)), dim3(nt), s, given);
             };
+            Parts q = cut_rows(given.n, given.vocab, given.work);
+            if (q.parts > 1) {
+                q.scores = (float *)(q.sums + given.n * q.parts);
+                const dim3 grid((unsigned)q.parts, (unsigned)given.n), one(1, (unsigned)given.n);
+                const hipError_t e = launch(k_distill_part<T>, grid, dim3(BLOCK), s, given, q);
+                if (e != hipSuccess) return e;
+                if (!given.grad)
+                    return given.k <= 256 ? launch(k_distill_rest<T, float, 256, false>, one, dim3(256), s, given, q)
+                                          : launch(k_distill_rest<T, float, 1024, false>, one, dim3(1024), s, given, q);
+                return given.k <= 256 ? launch(k_distill_rest<T, TO, 256, true>, grid, dim3(256), s, given, q)
+                                      : launch(k_distill_rest<T, TO, 1024, true>, grid, dim3(1024), s, given, q);
+            }
             const auto pick = [&](auto stream) {
                 constexpr bool S = decltype(stream)::value;
                 if (given.k <= 64 && units <= 64 * 4) return go(k_distill<T, TO, 64, 4, true, S>, 64, 20);

@@ -401,12 +401,13 @@ def empty_cache4(slots, dim, device="cuda"):
 
 
 def _shapes4(q, scales, dim, what):
-    if q.dim() != 2 or scales.dim() != 2 or q.dtype != torch.uint8 or scales.dtype != torch.uint8 \
-            or scales.shape[0] != q.shape[0] or q.shape[1] != 16 * scales.shape[1] or not scales.shape[1]:
-        raise _bad(f"{what} {tuple(q.shape)} {q.dtype}, scales {tuple(scales.shape)} {scales.dtype}: uint8 "
+    a, b = q.shape, scales.shape
+    if len(a) != 2 or len(b) != 2 or q.dtype != torch.uint8 or scales.dtype != torch.uint8 or b[0] != a[0] \
+            or a[1] != 16 * b[1] or not b[1]:
+        raise _bad(f"{what} {tuple(a)} {q.dtype}, scales {tuple(b)} {scales.dtype}: uint8 "
                    "[rows, dim / 2] and [rows, dim / 32] are needed, dim a multiple of 32")
-    if dim is not None and scales.shape[1] != _blocks(dim):
-        raise _bad(f"{what}: {scales.shape[1]} scales per row, {_blocks(dim)} are needed for {dim} columns")
+    if dim is not None and b[1] != _blocks(dim):
+        raise _bad(f"{what}: {b[1]} scales per row, {_blocks(dim)} are needed for {dim} columns")
 
 
 def _cache4(q, scales, dim):
@@ -480,17 +481,23 @@ def quantize4(x, stream=None):
 
 
 def _factor4(q, scales, what):
-    """A factor of product4, copied where its rows do not lie as the kernel reads them: bytes, their row
-    stride, scales, theirs."""
+    """A factor of product4, copied where its rows do not lie as the kernel reads them: bytes, scales, and
+    their addresses and row strides."""
     _shapes4(q, scales, None, what)
-    n, given = q.shape[0], []
-    for t, ld, most in zip((q, scales), _strides4(2 * q.shape[1]), (1 << 23, 1 << 40)):
+    n, width = q.shape
+    (ld, step), (sld, sstep) = q.stride(), scales.stride()
+    at, sat = q.data_ptr(), scales.data_ptr()
+    if (at | sat | ld | sld) % 16 == 0 and step == 1 and sstep == 1 and width <= ld < 1 << 23 and sld >= width // 16:
+        return q, scales, at, ld, sat, sld
+    given = []
+    for t, to, most in zip((q, scales), _strides4(2 * width), (1 << 23, 1 << 40)):
         width = t.shape[1]
         if t.data_ptr() % 16 or (width > 1 and t.stride(1) != 1) or (
                 n > 1 and not (width <= t.stride(0) < most and t.stride(0) % 16 == 0)):
-            t = torch.empty((n, ld), dtype=torch.uint8, device=t.device)[:, :width].copy_(t)
-        given += [t, t.stride(0) if n > 1 else ld]
-    return given
+            t = torch.empty((n, to), dtype=torch.uint8, device=t.device)[:, :width].copy_(t)
+        given.append((t, t.data_ptr(), t.stride(0) if n > 1 else to))
+    (q, at, ld), (scales, sat, sld) = given
+    return q, scales, at, ld, sat, sld
 
 
 def product4(x, x_scales, w, w_scales, dtype=torch.bfloat16, out=None, stream=None):
@@ -501,16 +508,17 @@ def product4(x, x_scales, w, w_scales, dtype=torch.bfloat16, out=None, stream=No
     if st is None:
         with _on(stream, x):
             return product4(x, x_scales, w, w_scales, dtype, out)
-    a, ald, xs, xsld = _factor4(x, x_scales, "x")
-    b, bld, ws, wsld = _factor4(w, w_scales, "w")
-    if a.shape[1] != b.shape[1]:
+    a, xs, at, ald, xat, xsld = _factor4(x, x_scales, "x")
+    b, ws, bt, bld, wat, wsld = _factor4(w, w_scales, "w")
+    (m, half), (n, same) = a.shape, b.shape
+    if half != same:
         raise _bad(f"x {tuple(x.shape)}, w {tuple(w.shape)}: [m, k / 2] and [n, k / 2] are needed")
     lib = _lib or _load()
-    m, n, k = a.shape[0], b.shape[0], 2 * a.shape[1]
+    k = 2 * half
     work = _workspace(lib.sp_product4_workspace, x.device, m, n, k)
     scores, to, old = _output(out, (m, n), dtype, x.device)
     _check(lib.sp_product4(
-        a.data_ptr(), xs.data_ptr(), m, ald, xsld, b.data_ptr(), ws.data_ptr(), n, bld, wsld, k, to,
+        at, xat, m, ald, xsld, bt, wat, n, bld, wsld, k, to,
         _type(_FLOAT, dtype, "out"), old, *((0, 0) if work is None else (work.data_ptr(), work.shape[0])), st))
     _changed(out)
     return scores
@@ -522,7 +530,10 @@ def _each_row(t, scores, width, what, dtypes):
     """What a call has for each row of scores, [*rows, width], or for all of them alike, [width]: the
     tensor, its address, its row stride (0: one row for all) and the number of its type."""
     code = _type(dtypes, t.dtype, what)
-    if t.dim() == 0 or (t.dim() > 1 and t.shape[:-1] != scores.shape[:-1]) or (width is not None and t.shape[-1] != width):
+    shape, of = t.shape, scores.shape
+    if len(shape) == 2 == len(of) and shape[0] == of[0] and width in (None, shape[1]) and t.is_contiguous():
+        return t, t.data_ptr(), shape[1], code
+    if not shape or (len(shape) > 1 and shape[:-1] != of[:-1]) or width not in (None, shape[-1]):
         raise _bad(f"{what} {tuple(t.shape)}, scores {tuple(scores.shape)}")
     if t.dim() == 1:
         t = _flat(t)
