@@ -533,7 +533,7 @@ sp_status sp_product4(const uint8_t *x, const uint8_t *x_scales, int64_t m, int6
  *   bias_tokens [n][biases], SP_I32 or SP_I64, and bias [n][biases] fp32: entries whose token is
  *     no column count nothing; biases 0: none.
  *   allowed [n][vocab / 32, rounded up]: column v is bit v % 32 of word v / 32 (NULL: all).
- * Strides of these four may be 0: one row for all.  vocab, length and biases: at most 2^20.
+ * Strides of these may be 0: one row for all.  vocab and length: at most 2^20; biases: at most 2047.
  */
 sp_status sp_adjust(const void *scores, int32_t type, int64_t n, int64_t vocab, int64_t ld,
                     const void *previous, int32_t previous_type, int64_t length, int64_t previous_ld,

@@ -24,6 +24,7 @@ constexpr int64_t MAX_WIDTH = 1 << 30;     // columns of dropout's rows
 constexpr int64_t MAX_LD = 1ll << 40;
 constexpr int64_t MAX_K = 131071;          // 128 * 128 * k stays within 32 bits
 constexpr int64_t MAX_LD4 = 1 << 23;       // 256 rows of 4 bits in 32 bits
+constexpr int64_t MAX_BIASES = 2047;       // a row's, 11 bits beside 21 of a count
 constexpr int64_t MAX_TEACHER = 1024;      // a teacher's entries of one row, in LDS
 
 sp_status bad(const char *fmt, ...) __attribute__((format(printf, 1, 2)));
@@ -339,7 +340,7 @@ extern "C" sp_status sp_adjust(const void *scores, int32_t type, int64_t n, int6
     if (n < 0 || n > MAX_N) return bad("%lld rows", (long long)n);
     if (vocab < 1 || vocab > MAX_DIM) return bad("%lld columns not in 1..%lld", (long long)vocab, (long long)MAX_DIM);
     if (length < 0 || length > MAX_DIM) return bad("%lld previous tokens not in 0..%lld", (long long)length, (long long)MAX_DIM);
-    if (biases < 0 || biases > MAX_DIM) return bad("%lld biases not in 0..%lld", (long long)biases, (long long)MAX_DIM);
+    if (biases < 0 || biases > MAX_BIASES) return bad("%lld biases not in 0..%lld", (long long)biases, (long long)MAX_BIASES);
     if (length > 0 && !is_index(previous_type)) return bad("previous tokens' type %d", previous_type);
     if (biases > 0 && !is_index(bias_type)) return bad("biases' token type %d", bias_type);
     if (!(repetition > 0.f && std::isfinite(repetition))) return bad("repetition %g is no positive number", (double)repetition);

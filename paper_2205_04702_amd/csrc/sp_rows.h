@@ -275,6 +275,67 @@ __device__ __forceinline__ void put_row_oct(T *row, int32_t oct, int32_t dim, bo
     store_oct<STREAM>(row + (int64_t)oct * OCT, left < OCT ? left : OCT, v);
 }
 
+// ---------------------------------------------------------------- units
+//
+// Rows of scores are worked on in units of 16 bytes, at any address, and the columns behind the last
+// whole unit one by one.  Units are loaded and stored through the row's buffer descriptor, whose bounds the
+// hardware checks: past the last unit a load gives zeros and a store does nothing, with no branch
+// around either, so that the waits for a thread's loads can be counted (across branches they became
+// waits for everything in flight, and loads and stores took turns).
+typedef uint32_t unit __attribute__((ext_vector_type(4)));
+
+template <typename T>
+constexpr int COLS = 16 / (int)sizeof(T);
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *row, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(row), 0, bytes, 0x00027000);
+}
+template <bool STREAM>
+__device__ __forceinline__ unit load_unit(__amdgpu_buffer_rsrc_t row, int32_t u)
+{
+    return __builtin_amdgcn_raw_buffer_load_b128(row, (uint32_t)u * 16, 0, STREAM ? 2 : 0);
+}
+template <typename T>
+__device__ __forceinline__ float column(const unit &x, int k)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(x[k]);
+    const uint16_t h = (uint16_t)(x[k / 2] >> (k % 2 * 16));
+    T v;
+    __builtin_memcpy(&v, &h, sizeof(T) < 4 ? sizeof v : 0);
+    return to_float(v);
+}
+template <typename T>
+__device__ __forceinline__ unit all_of(float x)
+{
+    const T v = from_float<T>(x);
+    uint32_t w = 0;
+    __builtin_memcpy(&w, &v, sizeof v);
+    if (sizeof(T) == 2) w |= w << 16;
+    return unit{w, w, w, w};
+}
+// Columns of a unit of the scores, as the output's type.
+template <bool STREAM, typename TO, int C>
+__device__ __forceinline__ void store_unit(__amdgpu_buffer_rsrc_t row, int32_t u, const float (&v)[C])
+{
+    Pack<TO, C> p;
+#pragma unroll
+    for (int k = 0; k < C; ++k) p.v[k] = from_float<TO>(v[k]);
+    constexpr int BYTES = (int)sizeof p, AUX = STREAM ? 2 : 0;
+    if constexpr (BYTES == 8) {
+        uint32_t w __attribute__((ext_vector_type(2)));
+        __builtin_memcpy(&w, &p, 8);
+        __builtin_amdgcn_raw_buffer_store_b64(w, row, (uint32_t)u * 8, 0, AUX);
+    } else {
+#pragma unroll
+        for (int i = 0; i < BYTES / 16; ++i) {
+            unit w;
+            __builtin_memcpy(&w, (const char *)&p + 16 * i, 16);
+            __builtin_amdgcn_raw_buffer_store_b128(w, row, (uint32_t)(u * BYTES + 16 * i), 0, AUX);
+        }
+    }
+}
+
 // ---------------------------------------------------------------- dropout
 //
 // Philox 4x32 with 10 rounds (Salmon, Moraes, Dror and Shaw, "Parallel random

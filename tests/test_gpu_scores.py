@@ -82,6 +82,7 @@ def adjusted(r, numbers, **kw):
     (7, 1000, 0, 0, False, False, BF16, torch.int64),
     (1, 20_000, 2, 2, True, False, BF16, torch.int32),
     (70, 512, 17, 9, True, True, F32, torch.int64),
+    (2, 3001, 40, 2047, False, True, BF16, torch.int32),
 ])
 def test_adjust(n, vocab, length, biases, mask, per_row, dtype, tokens):
     r, numbers = request(n, vocab, length, biases, mask, per_row, dtype, vocab, tokens), (1.3, 0.25, 0.125)

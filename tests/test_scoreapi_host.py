@@ -59,6 +59,7 @@ GRAD = dict(list(DISTILL.items())[:13] + [("weight", 1.0), ("weights", A), ("los
     ("sp_adjust", ADJUST, dict(vocab=(1 << 20) + 1, ld=1 << 21, out_ld=1 << 21), "columns"),
     ("sp_adjust", ADJUST, dict(length=-1), "previous tokens"),
     ("sp_adjust", ADJUST, dict(biases=-1), "biases"),
+    ("sp_adjust", ADJUST, dict(biases=2048, bias_tokens_ld=2048, bias_ld=2048), "biases"),
     ("sp_adjust", ADJUST, dict(previous_type=tk.SP_F32), "previous tokens' type"),
     ("sp_adjust", ADJUST, dict(bias_type=tk.SP_F32), "token type"),
     ("sp_adjust", ADJUST, dict(repetition=0.0), "repetition"),
