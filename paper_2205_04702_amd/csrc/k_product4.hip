@@ -14,11 +14,11 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-constexpr int KT = 64;         // bytes of a row in one step: 128 columns, 4 scales
-constexpr int STAGES = 4;      // steps that LDS holds
+constexpr int KT = 128;        // bytes of a row in one step: 256 columns, 8 scales
 constexpr int CHUNK = 16;      // bytes of one access: 32 columns, one scale
+constexpr int CPR = KT / CHUNK;  // chunks per row and step
+constexpr int SETS = CPR / 2;  // of factors in a step: 64 columns each
 constexpr int FP4 = 4;         // the matrix instruction's number of the format
-constexpr int SCALE_STEPS = 4; // steps whose scales are one chunk
 constexpr uint32_t GROUP = 8;  // columns of tiles that an XCD works through together
 
 __device__ __forceinline__ void to_lds(const uint8_t *src, uint8_t *dst)
@@ -28,27 +28,37 @@ __device__ __forceinline__ void to_lds(const uint8_t *src, uint8_t *dst)
         (__attribute__((address_space(3))) void *)dst, CHUNK, 0, 0);
 }
 
+// Scales of one side as the product reads them: eight bytes of a row for each step, in the caller's
+// rows (a step is 8 bytes on, a row its stride) or packed step by step (k_pack_scales).
+struct Scales4 {
+    const uint8_t *p;
+    int64_t row, step;
+};
+
 // ---------------------------------------------------------------- tiles
 //
 // A block computes BM x BN outputs, each wave WM x WN of them in 32 x 32 pieces, over steps of
-// 64 bytes of a row.  LDS holds four steps: the rows of the step three ahead are on their way
-// straight to LDS while one is multiplied, their loads issued one by one between the matrix
-// instructions.  A row's four chunks of a step are rotated among themselves by its number (chunk
-// c of row r sits at c ^ (r >> 2 & 3)), so that the 16 lanes that LDS serves at a time fall on
-// different banks.  The scales of four steps are one chunk of a row's scales: thread t loads
-// that of the tile's row t, with every fourth step, into one of two buffers.  w is the left factor
-// of the matrix instruction: its four consecutive rows per lane are four consecutive outputs.
-template <int BM, int BN, int WM, int WN, typename TO, bool PARTIAL>
-__global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product4(Product4Args a, int32_t tiles_n, uint32_t tiles_m, int32_t per_split)
+// 128 bytes of a row: a whole line, which comes from L2 once (in steps of 64 bytes a tile's lines
+// were gone from L1 before their second half was asked for).  LDS holds STAGES steps.  A step is four
+// sets of factors, each read from LDS while the set before is multiplied.  Before its last set a
+// step's buffer has been read by all: behind the barrier there the loads of the step STAGES
+// ahead go straight into it, one by one between the matrix instructions.  A row's eight
+// chunks are rotated among themselves by its number (chunk c of row r sits at c ^ (r >> 1 & 7)), so that
+// the 16 lanes that LDS serves at a time fall on different banks.  A lane's scales, eight bytes of
+// its row, come to registers a step ahead, and one byte permutation leaves those of its
+// half, a byte for each set.  w is the left factor of the matrix instruction: its four
+// consecutive rows per lane are four consecutive outputs.
+template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool PARTIAL>
+__global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
+    k_product4(Product4Args a, Scales4 sx, Scales4 sw, int32_t tiles_n, uint32_t tiles_m, int32_t per_split)
 {
     constexpr int NW = (BM / WM) * (BN / WN), NT = NW * WAVE;
-    constexpr int TM = WM / 32, TN = WN / 32;
-    constexpr int CPR = KT / CHUNK, RPL = WAVE / CPR;  // chunks per row, rows per load of a wave
-    constexpr int LOADS = (BM + BN) * CPR / NT;        // of a wave and step
-    static_assert(LOADS * NT == (BM + BN) * CPR && BM % (NW * RPL) == 0 && NT >= BM + BN, "whole loads");
+    constexpr int TM = WM / 32, TN = WN / 32, TF = TM + TN;
+    constexpr int RPL = WAVE / CPR;              // rows per load of a wave
+    constexpr int LOADS = (BM + BN) * CPR / NT;  // of a wave and step
+    static_assert(LOADS * NT == (BM + BN) * CPR && BM % (NW * RPL) == 0 && NW % 2 == 0, "whole loads");
     constexpr int BUF = (BM + BN) * KT;
     __shared__ __attribute__((aligned(16))) uint8_t sm[STAGES * BUF];
-    __shared__ __attribute__((aligned(16))) uint8_t sc[2 * NT * CHUNK];
     const int wave = wave_id(), lane = lane_id();
     uint32_t tile_m = 0, tile_n = blockIdx.x;
     if (tiles_m > 1) {
@@ -71,7 +81,7 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product4(Product4Arg
     };
     uint32_t place[LOADS];
     const int my_row = wave * RPL + lane / CPR;
-    const int my_chunk = (lane % CPR) ^ (my_row >> 2 & (CPR - 1));  // (RPL rows keep the rotation)
+    const int my_chunk = (lane % CPR) ^ (my_row >> 1 & (CPR - 1));  // (NW * RPL rows keep the rotation)
     static_assert(NW * RPL % 16 == 0, "a load's rows rotate as the first one's");
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
@@ -80,26 +90,34 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product4(Product4Arg
         place[i] = (uint32_t)at * (uint32_t)(is_x ? a.x_ld : a.w_ld) + (uint32_t)(my_chunk * CHUNK);
     }
     const uint8_t *xt = a.x + m0 * a.x_ld, *wt = a.w + n0 * a.w_ld;
-    const int t = (int)threadIdx.x;
-    const uint8_t *scale_row = t < BM ? a.xs + (m0 + clamped(true, t)) * a.xs_ld
-                                      : a.ws + (n0 + clamped(false, t - BM)) * a.ws_ld;
-    const auto fetch_scales = [&](int32_t step) {
-        to_lds(scale_row + step / SCALE_STEPS * CHUNK, sc + (step / SCALE_STEPS % 2 * NT + wave * WAVE) * CHUNK);
-    };
     // Load i of a step; chunks past the rows' last one take that one.
     const auto fetch = [&](int32_t step, int i) {
-        if (i == 0 && (step % SCALE_STEPS == 0 || step == first)) fetch_scales(step);
         const bool is_x = i * NW * RPL < BM;
         const int32_t chunk = step * CPR + my_chunk, back = chunk >= a.blocks ? chunk - (a.blocks - 1) : 0;
         to_lds((is_x ? xt : wt) + step * KT + (place[i] - (uint32_t)(back * CHUNK)),
                sm + step % STAGES * BUF + (i * NW + wave) * RPL * KT);
     };
-    // Every wave's loads but its last `open` are in LDS (a step's scales come before its rows), and
-    // every wave is done with the buffer that is filled next.
-    const auto landed = [](int open) {
-        if (open >= 2 * LOADS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
-        else if (open >= LOADS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // Scales: x's pieces, then w's.
+    const uint8_t *scale_row[TF];
+#pragma unroll
+    for (int i = 0; i < TF; ++i)
+        scale_row[i] = i < TM ? sx.p + (m0 + clamped(true, wm + i * 32 + lane % 32)) * sx.row
+                              : sw.p + (n0 + clamped(false, wn + (i - TM) * 32 + lane % 32)) * sw.row;
+    uint2 coming[TF];
+    uint32_t now[TF];
+    const auto fetch_scales = [&](int32_t step) {
+#pragma unroll
+        for (int i = 0; i < TF; ++i) coming[i] = *(const uint2 *)(scale_row[i] + step * (i < TM ? sx.step : sw.step));
+    };
+    const uint32_t half = lane / 32 ? 0x07050301u : 0x06040200u;
+    const auto take_scales = [&]() {
+#pragma unroll
+        for (int i = 0; i < TF; ++i) now[i] = __builtin_amdgcn_perm(coming[i].y, coming[i].x, half);
+    };
+    // All but the last OPEN of this wave's loads have arrived, and every wave is done with the buffer
+    // that is filled next.
+    const auto landed = [](auto open) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(open)::value) : "memory");
     };
 
     v16f acc[TM][TN];
@@ -110,46 +128,31 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product4(Product4Arg
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
 
-    // Two sets of factors in registers: while one is multiplied the next arrives from LDS, also
-    // over the edge of a step.  A step's four scales of a row are one word, whose bytes 0 and 2
-    // are those of the step's two sets once it is shifted by the lane's half.
-    constexpr int KS = KT / 32;
-    static_assert(KS == 2, "two sets");
-    v4i f[2][TM + TN];  // x's, then w's
-    uint32_t now[TM + TN], next_scales[TM + TN];
+    v4i f[2][TF];  // x's, then w's
     const uint8_t *xb = sm + (wm + lane % 32) * KT, *wb = sm + (BM + wn + lane % 32) * KT;
-    const uint8_t *xsb = sc + (wm + lane % 32) * CHUNK, *wsb = sc + (BM + wn + lane % 32) * CHUNK;
-    const auto read = [&](int32_t step, int ks, int i) {
-        const int at = step % STAGES * BUF + ((ks * 2 + lane / 32) ^ (lane >> 2 & (CPR - 1))) * CHUNK;
-        f[ks][i] = i < TM ? *(const v4i *)(xb + i * 32 * KT + at) : *(const v4i *)(wb + (i - TM) * 32 * KT + at);
-        if (ks == 0) {
-            const int s = step / SCALE_STEPS % 2 * NT * CHUNK + step % SCALE_STEPS * CPR;
-            next_scales[i] = i < TM ? *(const uint32_t *)(xsb + i * 32 * CHUNK + s)
-                                    : *(const uint32_t *)(wsb + (i - TM) * 32 * CHUNK + s);
-        }
+    const auto read = [&](int32_t step, int set, int i) {
+        const int at = step % STAGES * BUF + ((set * 2 + lane / 32) ^ (lane >> 1 & (CPR - 1))) * CHUNK;
+        f[set & 1][i] = i < TM ? *(const v4i *)(xb + i * 32 * KT + at) : *(const v4i *)(wb + (i - TM) * 32 * KT + at);
     };
-    const auto take_scales = [&]() {
-#pragma unroll
-        for (int i = 0; i < TM + TN; ++i) now[i] = next_scales[i] >> (lane / 32 * 8);
-    };
-    // Set ks multiplied.  Between the matrix instructions: the other set's reads (of step
-    // `next`), and the loads of step `ahead`; -1: none.
-    const auto multiply = [&](auto set, int32_t next, int32_t ahead) {
-        constexpr int ks = decltype(set)::value;
+    // A set multiplied.  Between the matrix instructions: the next set's reads (READS: of step `next`),
+    // and the loads of step `ahead` (FETCHES).
+    const auto multiply = [&](auto which, auto reads, int32_t next, auto fetches, int32_t ahead) {
+        constexpr int set = decltype(which)::value;
+        constexpr bool READS = decltype(reads)::value, FETCHES = decltype(fetches)::value;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int p = 0; p < TM * TN; ++p) {
-            const v4i &u = f[ks][TM + p % TN], &v = f[ks][p / TN];
+            const v4i &u = f[set & 1][TM + p % TN], &v = f[set & 1][p / TN];
             acc[p / TN][p % TN] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
                 v8i{u.x, u.y, u.z, u.w, 0, 0, 0, 0}, v8i{v.x, v.y, v.z, v.w, 0, 0, 0, 0}, acc[p / TN][p % TN], FP4, FP4,
-                2 * ks, (int)now[TM + p % TN], 2 * ks, (int)now[p / TN]);
+                set, (int)now[TM + p % TN], set, (int)now[p / TN]);
             __builtin_amdgcn_sched_barrier(0);
-            if (next >= 0) {
+            if constexpr (READS) {
 #pragma unroll
-                for (int i = 0; i < TM + TN; ++i)
-                    if (i * (TM * TN) / (TM + TN) == p) read(next, ks ^ 1, i);
+                for (int i = 0; i < TF; ++i)
+                    if (i * (TM * TN) / TF == p) read(next, (set + 1) % SETS, i);
             }
-            if (ahead >= 0) {
+            if constexpr (FETCHES) {
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i)
                     if (i * (TM * TN) / LOADS == p) fetch(ahead, i);
@@ -157,53 +160,76 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE) k_product4(Product4Arg
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
     constexpr std::integral_constant<int, 0> set0{};
     constexpr std::integral_constant<int, 1> set1{};
+    constexpr std::integral_constant<int, 2> set2{};
+    constexpr std::integral_constant<int, 3> set3{};
+    static_assert(SETS == 4, "four sets");
+    constexpr std::integral_constant<int, (STAGES - 1) * LOADS> but_first{};
+    // (at least as many came after the next step's: later steps' rows and this one's scales)
+    constexpr std::integral_constant<int, (STAGES - 2) * LOADS + TF> but_next{};
+
+    fetch_scales(first);
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s)
+    for (int s = 0; s < STAGES; ++s)
         if (first + s < steps) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) fetch(first + s, i);
         }
-    landed((steps - first < STAGES - 1 ? steps - first - 1 : STAGES - 2) * LOADS);
+    if (steps - first >= STAGES) landed(but_first);
+    else landed(set0);
 #pragma unroll
-    for (int i = 0; i < TM + TN; ++i) read(first, 0, i);
+    for (int i = 0; i < TF; ++i) read(first, 0, i);
     int32_t s = first;
-    for (; s + STAGES - 1 < steps; ++s) {
+    for (; s + STAGES < steps; ++s) {
         take_scales();
-        multiply(set0, s, s + STAGES - 1);
-        landed(2 * LOADS);
-        multiply(set1, s + 1, -1);
+        fetch_scales(s + 1);
+        multiply(set0, yes, s, no, 0);
+        multiply(set1, yes, s, no, 0);
+        multiply(set2, yes, s, no, 0);
+        landed(but_next);
+        multiply(set3, yes, s + 1, yes, s + STAGES);
     }
     for (; s + 1 < steps; ++s) {
         take_scales();
-        multiply(set0, s, -1);
-        landed(s + 2 < steps ? LOADS : 0);
-        multiply(set1, s + 1, -1);
+        fetch_scales(s + 1);
+        multiply(set0, yes, s, no, 0);
+        multiply(set1, yes, s, no, 0);
+        multiply(set2, yes, s, no, 0);
+        landed(set0);
+        multiply(set3, yes, s + 1, no, 0);
     }
-    take_scales();
-#pragma unroll
-    for (int i = 0; i < TM + TN; ++i) read(s, 1, i);
     // The last step: what lies past the rows' end counts nothing, its scales neither.
-    const int left = a.blocks - s * CPR - lane / 32;
-    const uint32_t mask = left > 2 ? 0xFF00FFu : left > 0 ? 0xFFu : 0u;
+    take_scales();
+    const int left = a.blocks - s * CPR - lane / 32, have = (a.blocks - s * CPR + 1) / 2;  // chunks of this lane's half; sets
+    const uint32_t mask = left > 6 ? ~0u : left > 4 ? 0xFFFFFFu : left > 2 ? 0xFFFFu : left > 0 ? 0xFFu : 0u;
 #pragma unroll
-    for (int i = 0; i < TM + TN; ++i) {
-        now[i] &= mask;
+    for (int i = 0; i < TF; ++i) now[i] &= mask;
+    const auto last_set = [&](auto which) {
+        constexpr int set = decltype(which)::value;
+        if (set >= have) return;  // the same for all
+        if (set > 0) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (left <= 0) f[0][i][q] = 0;
-            if (left <= 2) f[1][i][q] = 0;
+            for (int i = 0; i < TF; ++i) read(s, set, i);
         }
-    }
-    multiply(set0, -1, -1);
-    multiply(set1, -1, -1);
+        if (left <= 2 * set) {
+#pragma unroll
+            for (int i = 0; i < TF; ++i) f[set & 1][i] = v4i{0, 0, 0, 0};
+        }
+        multiply(which, no, 0, no, 0);
+    };
+    last_set(set0);
+    last_set(set1);
+    last_set(set2);
+    last_set(set3);
     __syncthreads();
 
     // Out through LDS, 32 rows at a time: a lane then has consecutive outputs of a row, 16
     // bytes of them, and a wave's store whole rows of its tile.
     constexpr int EP = 16 / (int)sizeof(TO);  // outputs per lane and store
-    constexpr int LPR = WN / EP;              // lanes per row
+    constexpr int LPR = WN / EP;              // lanes per row and store
     constexpr int STRIDE = WN * 4 + 16;
     static_assert(NW * 32 * STRIDE <= (int)sizeof sm && WAVE % LPR == 0, "staging fits the buffers");
     uint8_t *stage = sm + wave * 32 * STRIDE;
@@ -276,50 +302,85 @@ __global__ void __launch_bounds__(BLOCK) k_product4_join(Product4Args a, int32_t
     }
 }
 
+// Scales step by step: out[step][row] is the eight bytes of a row's step, zeros past its end.  A tile
+// then reads its rows' scales of a step in whole lines; in the caller's rows they are 8 bytes of a
+// line each, and as many lines as the factors themselves.
+__global__ void __launch_bounds__(BLOCK) k_pack_scales(const uint8_t *scales, int64_t ld, int64_t rows, int32_t blocks, uint2 *out)
+{
+    constexpr int ROWS = 64, STEPS = 16;  // of a block; 16 threads read a row's 128 bytes
+    __shared__ uint2 words[STEPS][ROWS + 1];
+    const int64_t row0 = (int64_t)blockIdx.x * ROWS;
+    const int32_t step0 = (int32_t)blockIdx.y * STEPS, steps = (blocks + CPR - 1) / CPR;
+    for (int i = (int)threadIdx.x; i < ROWS * STEPS; i += BLOCK) {
+        const int64_t row = row0 + i / STEPS;
+        const int32_t step = step0 + i % STEPS;
+        if (row >= rows || step >= steps) continue;
+        uint2 w = *(const uint2 *)(scales + row * ld + step * CPR);
+        const int left = blocks - step * CPR;
+        if (left < 8) {
+            w.y = left <= 4 ? 0u : w.y & ((1u << (8 * (left - 4))) - 1);
+            w.x = left >= 4 ? w.x : w.x & ((1u << (8 * left)) - 1);
+        }
+        words[i % STEPS][i / STEPS] = w;
+    }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < ROWS * STEPS; i += BLOCK) {
+        const int64_t row = row0 + i % ROWS;
+        const int32_t step = step0 + i / ROWS;
+        if (row < rows && step < steps) out[step * rows + row] = words[i / ROWS][i % ROWS];
+    }
+}
+
 // ---------------------------------------------------------------- host
+
+static int64_t steps_of(int32_t blocks) { return (blocks + CPR - 1) / CPR; }
+
+// Packed scales pay for themselves where many tiles read them.
+static bool packs(int64_t m, int64_t n, const Cut &c) { return c.tile == 0 && c.splits == 1; }
 
 int64_t product4_workspace(int64_t m, int64_t n, int32_t blocks)
 {
     if (m == 0 || n == 0) return 0;
     const Cut c = cut_product(m, n, (int64_t)blocks * CHUNK);
-    return c.splits > 1 ? m * n * 4 * c.splits : 0;
+    return c.splits > 1 ? m * n * 4 * c.splits : packs(m, n, c) ? steps_of(blocks) * 8 * (m + n) : 0;
 }
 
-template <int BM, int BN, int WM, int WN, typename TO, bool PARTIAL>
-static hipError_t run_tiles(const Product4Args &a, int32_t splits, hipStream_t s)
+template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool PARTIAL>
+static hipError_t run_tiles(const Product4Args &a, const Scales4 &sx, const Scales4 &sw, int32_t splits, hipStream_t s)
 {
     const int64_t tm = (a.m + BM - 1) / BM, tn = (a.n + BN - 1) / BN;
     if (tm * tn > LAUNCH_BLOCKS / 2) {  // (up to 512 threads each; never in parts of k)
         Product4Args lo = a, hi = a;
+        Scales4 hx = sx, hw = sw;
         if (tm >= tn) {
             lo.m = tm / 2 * BM;
             hi.m = a.m - lo.m;
             hi.x += lo.m * a.x_ld;
-            hi.xs += lo.m * a.xs_ld;
+            hx.p += lo.m * sx.row;
             hi.out = (TO *)a.out + lo.m * a.out_ld;
         } else {
             lo.n = tn / 2 * BN;
             hi.n = a.n - lo.n;
             hi.w += lo.n * a.w_ld;
-            hi.ws += lo.n * a.ws_ld;
+            hw.p += lo.n * sw.row;
             hi.out = (TO *)a.out + lo.n;
         }
-        const hipError_t r = run_tiles<BM, BN, WM, WN, TO, PARTIAL>(lo, splits, s);
-        return r != hipSuccess ? r : run_tiles<BM, BN, WM, WN, TO, PARTIAL>(hi, splits, s);
+        const hipError_t r = run_tiles<BM, BN, WM, WN, STAGES, TO, PARTIAL>(lo, sx, sw, splits, s);
+        return r != hipSuccess ? r : run_tiles<BM, BN, WM, WN, STAGES, TO, PARTIAL>(hi, hx, hw, splits, s);
     }
-    const int32_t steps = (a.blocks + KT / CHUNK - 1) / (KT / CHUNK), per = (steps + splits - 1) / splits;
+    const int32_t steps = (int32_t)steps_of(a.blocks), per = (steps + splits - 1) / splits;
     const dim3 grid((unsigned)(tm * tn), (unsigned)((steps + per - 1) / per)), block(BM / WM * (BN / WN) * WAVE);
-    return launch(k_product4<BM, BN, WM, WN, TO, PARTIAL>, grid, block, s, a, (int32_t)tn, (uint32_t)tm, per);
+    return launch(k_product4<BM, BN, WM, WN, STAGES, TO, PARTIAL>, grid, block, s, a, sx, sw, (int32_t)tn, (uint32_t)tm, per);
 }
 
 template <typename TO, bool PARTIAL>
-static hipError_t run_cut(const Product4Args &a, const Cut &c, hipStream_t s)
+static hipError_t run_cut(const Product4Args &a, const Scales4 &sx, const Scales4 &sw, const Cut &c, hipStream_t s)
 {
-    return c.tile == 0   ? run_tiles<256, 256, 128, 64, TO, PARTIAL>(a, c.splits, s)
-           : c.tile == 1 ? run_tiles<128, 128, 64, 64, TO, PARTIAL>(a, c.splits, s)
-           : c.tile == 2 ? run_tiles<64, 128, 32, 64, TO, PARTIAL>(a, c.splits, s)
-           : c.tile == 3 ? run_tiles<64, 64, 32, 32, TO, PARTIAL>(a, c.splits, s)
-                         : run_tiles<32, 64, 32, 32, TO, PARTIAL>(a, c.splits, s);
+    return c.tile == 0   ? run_tiles<256, 256, 128, 128, 2, TO, PARTIAL>(a, sx, sw, c.splits, s)
+           : c.tile == 1 ? run_tiles<128, 128, 64, 64, 4, TO, PARTIAL>(a, sx, sw, c.splits, s)
+           : c.tile == 2 ? run_tiles<64, 128, 32, 64, 3, TO, PARTIAL>(a, sx, sw, c.splits, s)
+           : c.tile == 3 ? run_tiles<64, 64, 32, 32, 4, TO, PARTIAL>(a, sx, sw, c.splits, s)
+                         : run_tiles<32, 64, 32, 32, 4, TO, PARTIAL>(a, sx, sw, c.splits, s);
 }
 
 hipError_t run_product4(const Product4Args &given, hipStream_t s)
@@ -328,14 +389,27 @@ hipError_t run_product4(const Product4Args &given, hipStream_t s)
     if (a.m == 1) a.x_ld = a.xs_ld = 0;  // the stride of a single row is never used
     if (a.n == 1) a.w_ld = a.ws_ld = 0;
     const Cut c = cut_product(a.m, a.n, (int64_t)a.blocks * CHUNK);
+    Scales4 sx{a.xs, a.xs_ld, CPR}, sw{a.ws, a.ws_ld, CPR};
+    if (packs(a.m, a.n, c)) {
+        const auto pack = [&](Scales4 &side, int64_t rows, uint2 *to) {
+            const dim3 grid((unsigned)((rows + 63) / 64), (unsigned)((steps_of(a.blocks) + 15) / 16));
+            const hipError_t e = launch(k_pack_scales, grid, dim3(BLOCK), s, side.p, side.row, rows, a.blocks, to);
+            side = Scales4{(const uint8_t *)to, 8, rows * 8};
+            return e;
+        };
+        uint2 *to = (uint2 *)a.work;
+        hipError_t e = pack(sx, a.m, to);
+        if (e == hipSuccess) e = pack(sw, a.n, to + steps_of(a.blocks) * a.m);
+        if (e != hipSuccess) return e;
+    }
     return with_type(a.out_type, [&](auto to) {
         using TO = decltype(to);
-        if (c.splits == 1) return run_cut<TO, false>(a, c, s);
+        if (c.splits == 1) return run_cut<TO, false>(a, sx, sw, c, s);
         Product4Args p = a;
         p.out_ld = a.n;
-        hipError_t r = run_cut<float, true>(p, c, s);
+        hipError_t r = run_cut<float, true>(p, sx, sw, c, s);
         if (r != hipSuccess) return r;
-        const int32_t steps = (a.blocks + KT / CHUNK - 1) / (KT / CHUNK), per = (steps + c.splits - 1) / c.splits;
+        const int32_t steps = (int32_t)steps_of(a.blocks), per = (steps + c.splits - 1) / c.splits;
         const int64_t blocks = (a.m * a.n + 4 * BLOCK - 1) / (4 * BLOCK);
         if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
         return launch(k_product4_join<TO>, dim3((unsigned)blocks), dim3(BLOCK), s, a, (steps + per - 1) / per);
