@@ -509,7 +509,7 @@ sp_status sp_cache4_read(const uint8_t *q, int64_t slots, int64_t dim, int64_t q
  * rounded up to a multiple of 32: what the last block holds past k counts, so zeros).  Products and
  * scales are exact, sums fp32.  A scale byte of 255 gives NaN.  Rows of x, of w and of their scales
  * start at multiples of 16 bytes (x and w best of 128), and are read in whole aligned 16-byte
- * pieces (scales past the row's last count nothing); strides of x and w are below 2^23.
+ * pieces (scales past the row's last count nothing); their strides and the output's are below 2^23.
  * out: SP_F32, SP_BF16 or SP_F16.  workspace: as for sp_lookup_grad, of the bytes that
  * sp_product4_workspace gives for m, n and k.
  */

@@ -18,14 +18,14 @@ constexpr int KT = 128;        // bytes of a row in one step: 256 columns, 8 sca
 constexpr int CHUNK = 16;      // bytes of one access: 32 columns, one scale
 constexpr int CPR = KT / CHUNK;  // chunks per row and step
 constexpr int SETS = CPR / 2;  // of factors in a step: 64 columns each
+constexpr int64_t CUS = 256, LDS_BYTES = 160 * 1024;
 constexpr int FP4 = 4;         // the matrix instruction's number of the format
 constexpr uint32_t GROUP = 8;  // columns of tiles that an XCD works through together
 
-__device__ __forceinline__ void to_lds(const uint8_t *src, uint8_t *dst)
+// 16 bytes a lane, straight to LDS, at `at` plus the wave's `from` in a buffer; zeros past its end.
+__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t rows, uint32_t at, uint32_t from, uint8_t *dst)
 {
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void *)src,
-        (__attribute__((address_space(3))) void *)dst, CHUNK, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void *)dst, CHUNK, at, from, 0, 0);
 }
 
 // Scales of one side as the product reads them: eight bytes of a row for each step, in the caller's
@@ -37,16 +37,17 @@ struct Scales4 {
 
 // ---------------------------------------------------------------- tiles
 //
-// A block computes BM x BN outputs, each wave WM x WN of them in 32 x 32 pieces, over steps of
+// A block computes tiles of BM x BN outputs, each wave WM x WN of them in 32 x 32 pieces, over steps of
 // 128 bytes of a row: a whole line, which comes from L2 once (in steps of 64 bytes a tile's lines
 // were gone from L1 before their second half was asked for).  LDS holds STAGES steps.  A step is four
 // sets of factors, each read from LDS while the set before is multiplied.  Before its last set a
 // step's buffer has been read by all: behind the barrier there the loads of the step STAGES
-// ahead go straight into it, one by one between the matrix instructions.  A row's eight
-// chunks are rotated among themselves by its number (chunk c of row r sits at c ^ (r >> 1 & 7)), so that
-// the 16 lanes that LDS serves at a time fall on different banks.  A lane's scales, eight bytes of
-// its row, come to registers a step ahead, and one byte permutation leaves those of its
-// half, a byte for each set.  w is the left factor of the matrix instruction: its four
+// ahead go straight into it, one by one between the matrix instructions.  The steps of a block's tiles
+// follow each other without a gap: while a tile is stored, the next one's first steps are on their way.
+// A row's eight chunks are rotated among themselves by its number (chunk c of row r sits at
+// c ^ (r >> 1 & 7)), so that the 16 lanes that LDS serves at a time fall on different banks.  A
+// lane's scales, eight bytes of its row, come to registers a step ahead, and one byte permutation leaves
+// those of its half, a byte for each set.  w is the left factor of the matrix instruction: its four
 // consecutive rows per lane are four consecutive outputs.
 template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool PARTIAL>
 __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
@@ -60,85 +61,115 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
     constexpr int BUF = (BM + BN) * KT;
     __shared__ __attribute__((aligned(16))) uint8_t sm[STAGES * BUF];
     const int wave = wave_id(), lane = lane_id();
-    uint32_t tile_m = 0, tile_n = blockIdx.x;
-    if (tiles_m > 1) {
-        const uint32_t tile = (uint32_t)xcd_block(blockIdx.x, gridDim.x);
-        const uint32_t group = tile / (GROUP * tiles_m), in = tile - group * GROUP * tiles_m;
-        const uint32_t wide = (uint32_t)tiles_n - group * GROUP < GROUP ? (uint32_t)tiles_n - group * GROUP : GROUP;
-        tile_m = in / wide;
-        tile_n = group * GROUP + in % wide;
-    }
-    const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
-    const int32_t first = (int32_t)blockIdx.y * per_split;
-    const int32_t all = (a.blocks + CPR - 1) / CPR, steps = first + per_split < all ? first + per_split : all;
-    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
-
-    // This lane's chunk of each load: a place relative to the tile's first row (strides are below
-    // 2^23, so it fits 32 bits); rows past the last take that one.
-    const auto clamped = [&](bool is_x, int64_t row) {
-        const int64_t last = is_x ? a.m - 1 - m0 : a.n - 1 - n0;
-        return row < last ? row : last;
+    const uint32_t tiles = (uint32_t)tiles_n * tiles_m;
+    const auto tile_at = [&](uint32_t i, int64_t &m0, int64_t &n0) {
+        uint32_t tile_m = 0, tile_n = i;
+        if (tiles_m > 1) {
+            const uint32_t tile = (uint32_t)xcd_block(i, tiles);
+            const uint32_t group = tile / (GROUP * tiles_m), in = tile - group * GROUP * tiles_m;
+            const uint32_t wide = (uint32_t)tiles_n - group * GROUP < GROUP ? (uint32_t)tiles_n - group * GROUP : GROUP;
+            tile_m = in / wide;
+            tile_n = group * GROUP + in % wide;
+        }
+        m0 = (int64_t)tile_m * BM;
+        n0 = (int64_t)tile_n * BN;
     };
-    uint32_t place[LOADS];
+    const int32_t first = (int32_t)blockIdx.y * per_split;
+    const int32_t all = (a.blocks + CPR - 1) / CPR, end = first + per_split < all ? first + per_split : all;
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+    const auto row_at = [](int64_t row, int64_t last) { return (uint32_t)(row < last ? row : last); };
+
+    // What is loaded next: rows of a tile, a step.  The rows are buffers from the tile's first one on, whose
+    // bounds the hardware checks (strides are below 2^23, so they fit 32 bits): rows past the last are
+    // zeros, and so is everything once nothing is left to load.  Bytes behind a row's last chunk are its
+    // neighbour's; their scales are zeros, so they count nothing (2^-254 times a finite value is below
+    // anything that fp32 holds).
+    uint32_t load_tile = blockIdx.x;
+    int32_t load_step = first;
+    __amdgpu_buffer_rsrc_t x_rows, w_rows;
     const int my_row = wave * RPL + lane / CPR;
     const int my_chunk = (lane % CPR) ^ (my_row >> 1 & (CPR - 1));  // (NW * RPL rows keep the rotation)
     static_assert(NW * RPL % 16 == 0, "a load's rows rotate as the first one's");
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
+    const uint32_t x_at = (uint32_t)(my_row * (int)a.x_ld + my_chunk * CHUNK), w_at = (uint32_t)(my_row * (int)a.w_ld + my_chunk * CHUNK);
+    const auto rows_of = [&](const uint8_t *p, int64_t ld, int64_t rows, int most) {
+        if (rows > most) rows = most;
+        return buffer(p, rows > 0 ? (uint32_t)((rows - 1) * ld + a.blocks * CHUNK) : 0);
+    };
+    const auto aim = [&]() {
+        int64_t m0 = 0, n0 = 0;
+        const bool more = load_tile < tiles;
+        if (more) tile_at(load_tile, m0, n0);
+        x_rows = rows_of(a.x + m0 * a.x_ld, a.x_ld, more ? a.m - m0 : 0, BM);
+        w_rows = rows_of(a.w + n0 * a.w_ld, a.w_ld, more ? a.n - n0 : 0, BN);
+    };
+    const auto fetch = [&](int32_t stage, int i) {  // load i, into a stage
         const bool is_x = i * NW * RPL < BM;
-        const int64_t at = clamped(is_x, i * NW * RPL + my_row - (is_x ? 0 : BM));
-        place[i] = (uint32_t)at * (uint32_t)(is_x ? a.x_ld : a.w_ld) + (uint32_t)(my_chunk * CHUNK);
-    }
-    const uint8_t *xt = a.x + m0 * a.x_ld, *wt = a.w + n0 * a.w_ld;
-    // Load i of a step; chunks past the rows' last one take that one.
-    const auto fetch = [&](int32_t step, int i) {
-        const bool is_x = i * NW * RPL < BM;
-        const int32_t chunk = step * CPR + my_chunk, back = chunk >= a.blocks ? chunk - (a.blocks - 1) : 0;
-        to_lds((is_x ? xt : wt) + step * KT + (place[i] - (uint32_t)(back * CHUNK)),
-               sm + step % STAGES * BUF + (i * NW + wave) * RPL * KT);
+        const int rows = i * NW * RPL - (is_x ? 0 : BM);
+        to_lds(is_x ? x_rows : w_rows, is_x ? x_at : w_at, (uint32_t)(rows * (int)(is_x ? a.x_ld : a.w_ld) + load_step * KT),
+               sm + stage * BUF + (i * NW + wave) * RPL * KT);
+    };
+    const auto fetched = [&]() {  // on to the next step, or tile
+        if (++load_step < end) return;
+        load_step = first;
+        load_tile += gridDim.x;
+        aim();
     };
     // Scales: x's pieces, then w's.
-    const uint8_t *scale_row[TF];
+    const uint8_t *xs, *ws;
+    uint32_t scale_place[TF];
+    const auto aim_scales = [&](int64_t m0, int64_t n0) {
+        int l = lane % 32;
+        asm volatile("" : "+v"(l));
+        xs = sx.p + m0 * sx.row;
+        ws = sw.p + n0 * sw.row;
 #pragma unroll
-    for (int i = 0; i < TF; ++i)
-        scale_row[i] = i < TM ? sx.p + (m0 + clamped(true, wm + i * 32 + lane % 32)) * sx.row
-                              : sw.p + (n0 + clamped(false, wn + (i - TM) * 32 + lane % 32)) * sw.row;
+        for (int i = 0; i < TF; ++i)
+            scale_place[i] = i < TM ? row_at(wm + i * 32 + l, a.m - 1 - m0) * (uint32_t)sx.row
+                                    : row_at(wn + (i - TM) * 32 + l, a.n - 1 - n0) * (uint32_t)sw.row;
+    };
     uint2 coming[TF];
     uint32_t now[TF];
-    const auto fetch_scales = [&](int32_t step) {
-#pragma unroll
-        for (int i = 0; i < TF; ++i) coming[i] = *(const uint2 *)(scale_row[i] + step * (i < TM ? sx.step : sw.step));
+    const auto fetch_scale = [&](int32_t step, int i) {
+        coming[i] = *(const uint2 *)((i < TM ? xs + step * sx.step : ws + step * sw.step) + scale_place[i]);
     };
     const uint32_t half = lane / 32 ? 0x07050301u : 0x06040200u;
-    const auto take_scales = [&]() {
+    const auto take_scales = [&](int32_t step) {
 #pragma unroll
         for (int i = 0; i < TF; ++i) now[i] = __builtin_amdgcn_perm(coming[i].y, coming[i].x, half);
+        if (step + 1 == all) {  // none past the rows' end
+            const int left = a.blocks - step * CPR - lane / 32;
+            const uint32_t mask = left > 6 ? ~0u : left > 4 ? 0xFFFFFFu : left > 2 ? 0xFFFFu : left > 0 ? 0xFFu : 0u;
+#pragma unroll
+            for (int i = 0; i < TF; ++i) now[i] &= mask;
+        }
     };
-    // All but the last OPEN of this wave's loads have arrived, and every wave is done with the buffer
-    // that is filled next.
+    // All but the last OPEN of this wave's loads and stores are done, and every wave is done with the
+    // buffer that is filled next.
     const auto landed = [](auto open) {
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(open)::value) : "memory");
     };
 
     v16f acc[TM][TN];
+    const auto clear = [&]() {
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+                for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+    };
 
     v4i f[2][TF];  // x's, then w's
     const uint8_t *xb = sm + (wm + lane % 32) * KT, *wb = sm + (BM + wn + lane % 32) * KT;
-    const auto read = [&](int32_t step, int set, int i) {
-        const int at = step % STAGES * BUF + ((set * 2 + lane / 32) ^ (lane >> 1 & (CPR - 1))) * CHUNK;
+    const auto read = [&](int32_t stage, int set, int i) {
+        const int at = stage * BUF + ((set * 2 + lane / 32) ^ (lane >> 1 & (CPR - 1))) * CHUNK;
         f[set & 1][i] = i < TM ? *(const v4i *)(xb + i * 32 * KT + at) : *(const v4i *)(wb + (i - TM) * 32 * KT + at);
     };
-    // A set multiplied.  Between the matrix instructions: the next set's reads (READS: of step `next`),
-    // and the loads of step `ahead` (FETCHES).
-    const auto multiply = [&](auto which, auto reads, int32_t next, auto fetches, int32_t ahead) {
+    // A set multiplied.  Between the matrix instructions: the next set's reads (READS: from `stage`), the
+    // scales of step `step` (SCALES), and the loads of the step that is loaded next (FETCHES: into `into`).
+    const auto multiply = [&](auto which, auto reads, int32_t stage, auto scales, int32_t step, auto fetches, int32_t into) {
         constexpr int set = decltype(which)::value;
-        constexpr bool READS = decltype(reads)::value, FETCHES = decltype(fetches)::value;
+        constexpr bool READS = decltype(reads)::value, SCALES = decltype(scales)::value, FETCHES = decltype(fetches)::value;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int p = 0; p < TM * TN; ++p) {
@@ -147,19 +178,97 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
                 v8i{u.x, u.y, u.z, u.w, 0, 0, 0, 0}, v8i{v.x, v.y, v.z, v.w, 0, 0, 0, 0}, acc[p / TN][p % TN], FP4, FP4,
                 set, (int)now[TM + p % TN], set, (int)now[p / TN]);
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (READS) {
 #pragma unroll
-                for (int i = 0; i < TF; ++i)
-                    if (i * (TM * TN) / TF == p) read(next, (set + 1) % SETS, i);
-            }
+            for (int i = 0; i < TF; ++i)
+                if (i * (TM * TN) / TF == p) {
+                    if constexpr (READS) read(stage, (set + 1) % SETS, i);
+                    if constexpr (SCALES) fetch_scale(step, i);
+                }
             if constexpr (FETCHES) {
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i)
-                    if (i * (TM * TN) / LOADS == p) fetch(ahead, i);
+                    if (i * (TM * TN) / LOADS == p) fetch(into, i);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        // (else the compiler takes the multiplications of all four sets behind the step's branches)
+#pragma unroll
+        for (int p = 0; p < TM * TN; ++p) asm volatile("" : "+a"(acc[p / TN][p % TN]));
     };
+    // A tile's outputs, straight from the registers: two lanes' halves of eight columns are exchanged where
+    // they are 16 bits wide, so that each store is 16 bytes a lane.  32 rows are a buffer (strides are below
+    // 2^23), and a store that is not wholly inside the output is aimed past its end, so that there are as
+    // many stores everywhere; where a row's last one is not whole (`ragged`) they go column by column.
+    // Sums are taken out of their registers one by one: left to the compiler they were all moved at once,
+    // and what the next tile needs went to memory for them.
+    const auto sum = [](float x) {
+        float v;
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(x));
+        return v;
+    };
+    constexpr int EP = 16 / (int)sizeof(TO), STORES = TM * TN * 16 / EP;  // outputs of a lane and store; stores of a tile
+    const auto store = [&](int64_t m0, int64_t n0) {
+        constexpr uint32_t NOWHERE = 0xFFFFFF00u;
+        TO *base = (PARTIAL ? (TO *)a.work + (int64_t)blockIdx.y * a.m * a.n : (TO *)a.out) + n0 + wn;
+        const int64_t right = a.n - n0 - wn, down = a.m - m0 - wm;
+        int l = lane;
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");  // (the last matrix instruction's result, which `sum` reads)
+        asm volatile("" : "+v"(l));  // (else every store's place is worked out before the first tile and kept)
+        const int32_t columns = (int32_t)(right < WN ? right : WN), col = l / 32 * EP;
+        const uint32_t ld = (uint32_t)a.out_ld * (uint32_t)sizeof(TO), at = (uint32_t)(l % 32) * ld + (uint32_t)(col * (int)sizeof(TO));
+        const bool ragged = right < WN && right % EP != 0;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int32_t rows = (int32_t)(down - i * 32 < 32 ? down - i * 32 : 32);
+            const __amdgpu_buffer_rsrc_t to = buffer(base + (m0 + wm + i * 32) * a.out_ld, rows > 0 && columns > 0 ? (uint32_t)(rows - 1) * ld + (uint32_t)(columns * (int)sizeof(TO)) : 0);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; q += EP / 4) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    Pack<TO, EP> o;
+                    if constexpr (EP == 4) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) o.v[c] = from_float<TO>(sum(acc[i][j][q * 4 + c]));
+                    } else {
+                        Pack<TO, 4> lo, hi;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            lo.v[c] = from_float<TO>(sum(acc[i][j][q * 4 + c]));
+                            hi.v[c] = from_float<TO>(sum(acc[i][j][q * 4 + 4 + c]));
+                        }
+                        uint32_t x[2], y[2];
+                        __builtin_memcpy(x, &lo, 8);
+                        __builtin_memcpy(y, &hi, 8);
+                        const auto s0 = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
+                        const auto s1 = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
+                        const uint32_t w[4] = {s0[0], s1[0], s0[1], s1[1]};
+                        __builtin_memcpy(&o, w, 16);
+                    }
+                    const int32_t left = columns - col - (j * 32 + q * 8);
+                    constexpr uint32_t SIZE = (uint32_t)sizeof(TO);
+                    const uint32_t here = at + (uint32_t)(j * 32 + q * 8) * SIZE;
+                    if (!ragged) {
+                        unit w;
+                        __builtin_memcpy(&w, &o, 16);
+                        __builtin_amdgcn_raw_buffer_store_b128(w, to, left >= EP ? here : NOWHERE, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < EP; ++c) {
+                            const uint32_t to_column = c < left ? here + (uint32_t)c * SIZE : NOWHERE;
+                            if constexpr (SIZE == 4) {
+                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint((float)o.v[c]), to, to_column, 0, 0);
+                            } else {
+                                uint16_t h;
+                                __builtin_memcpy(&h, &o.v[c], 2);
+                                __builtin_amdgcn_raw_buffer_store_b16(h, to, to_column, 0, 0);
+                            }
+                        }
+                    }
+                }
+        }
+    };
+
     constexpr std::true_type yes{};
     constexpr std::false_type no{};
     constexpr std::integral_constant<int, 0> set0{};
@@ -167,110 +276,58 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
     constexpr std::integral_constant<int, 2> set2{};
     constexpr std::integral_constant<int, 3> set3{};
     static_assert(SETS == 4, "four sets");
+    // (At least as many came after the next step's: later steps' rows, this one's scales, a tile's stores.)
+    constexpr int OPEN = (STAGES - 2) * LOADS + TF;
     constexpr std::integral_constant<int, (STAGES - 1) * LOADS> but_first{};
-    // (at least as many came after the next step's: later steps' rows and this one's scales)
-    constexpr std::integral_constant<int, (STAGES - 2) * LOADS + TF> but_next{};
+    constexpr std::integral_constant<int, OPEN> but_next{};
+    constexpr std::integral_constant<int, OPEN + STORES < 63 ? OPEN + STORES : 63> but_stores{};
 
-    fetch_scales(first);
+    uint32_t tile = blockIdx.x;
+    int64_t m0, n0;
+    tile_at(tile, m0, n0);
+    aim();
+    aim_scales(m0, n0);
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s)
-        if (first + s < steps) {
+    for (int i = 0; i < TF; ++i) fetch_scale(first, i);
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) fetch(first + s, i);
-        }
-    if (steps - first >= STAGES) landed(but_first);
-    else landed(set0);
+    for (int s = 0; s < STAGES; ++s) {
 #pragma unroll
-    for (int i = 0; i < TF; ++i) read(first, 0, i);
-    int32_t s = first;
-    for (; s + STAGES < steps; ++s) {
-        take_scales();
-        fetch_scales(s + 1);
-        multiply(set0, yes, s, no, 0);
-        multiply(set1, yes, s, no, 0);
-        multiply(set2, yes, s, no, 0);
-        landed(but_next);
-        multiply(set3, yes, s + 1, yes, s + STAGES);
+        for (int i = 0; i < LOADS; ++i) fetch(s, i);
+        fetched();
     }
-    for (; s + 1 < steps; ++s) {
-        take_scales();
-        fetch_scales(s + 1);
-        multiply(set0, yes, s, no, 0);
-        multiply(set1, yes, s, no, 0);
-        multiply(set2, yes, s, no, 0);
-        landed(set0);
-        multiply(set3, yes, s + 1, no, 0);
-    }
-    // The last step: what lies past the rows' end counts nothing, its scales neither.
-    take_scales();
-    const int left = a.blocks - s * CPR - lane / 32, have = (a.blocks - s * CPR + 1) / 2;  // chunks of this lane's half; sets
-    const uint32_t mask = left > 6 ? ~0u : left > 4 ? 0xFFFFFFu : left > 2 ? 0xFFFFu : left > 0 ? 0xFFu : 0u;
+    landed(but_first);
 #pragma unroll
-    for (int i = 0; i < TF; ++i) now[i] &= mask;
-    const auto last_set = [&](auto which) {
-        constexpr int set = decltype(which)::value;
-        if (set >= have) return;  // the same for all
-        if (set > 0) {
-#pragma unroll
-            for (int i = 0; i < TF; ++i) read(s, set, i);
-        }
-        if (left <= 2 * set) {
-#pragma unroll
-            for (int i = 0; i < TF; ++i) f[set & 1][i] = v4i{0, 0, 0, 0};
-        }
-        multiply(which, no, 0, no, 0);
-    };
-    last_set(set0);
-    last_set(set1);
-    last_set(set2);
-    last_set(set3);
-    __syncthreads();
-
-    // Out through LDS, 32 rows at a time: a lane then has consecutive outputs of a row, 16
-    // bytes of them, and a wave's store whole rows of its tile.
-    constexpr int EP = 16 / (int)sizeof(TO);  // outputs per lane and store
-    constexpr int LPR = WN / EP;              // lanes per row and store
-    constexpr int STRIDE = WN * 4 + 16;
-    static_assert(NW * 32 * STRIDE <= (int)sizeof sm && WAVE % LPR == 0, "staging fits the buffers");
-    uint8_t *stage = sm + wave * 32 * STRIDE;
-    const int64_t n = n0 + wn + lane % LPR * EP;
-    TO *out = (PARTIAL ? (TO *)a.work + (int64_t)blockIdx.y * a.m * a.n : (TO *)a.out) + (m0 + wm + lane / LPR) * a.out_ld + n;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                Pack<float, 4> v;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v.v[c] = acc[i][j][q * 4 + c];
-                __builtin_memcpy(
-                    __builtin_assume_aligned(
-                        stage + lane % 32 * STRIDE + (j * 32 + q * 8 + lane / 32 * 4) * 4, 16),
-                    &v, sizeof v);
+    for (int i = 0; i < TF; ++i) read(0, 0, i);
+    int32_t stage = 0;
+    bool stored = false;  // a tile, just before
+    for (;;) {
+        const int64_t m = m0, n = n0;
+        const bool more = tile + gridDim.x < tiles;
+        int32_t step = first;
+        clear();
+        do {
+            const int32_t after = stage + 1 < STAGES ? stage + 1 : 0;
+            take_scales(step);
+            if (step + 1 == end && more) {  // the next step's scales are another tile's
+                tile += gridDim.x;
+                tile_at(tile, m0, n0);
+                aim_scales(m0, n0);
             }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int r0 = 0; r0 < 32; r0 += WAVE / LPR) {
-            Pack<float, EP> v;
-            __builtin_memcpy(&v, __builtin_assume_aligned(stage + (r0 + lane / LPR) * STRIDE +
-                                                              lane % LPR * EP * 4, 16),
-                             sizeof v);
-            Pack<TO, EP> o;
-#pragma unroll
-            for (int c = 0; c < EP; ++c) o.v[c] = from_float<TO>(v.v[c]);
-            TO *p = out + (int64_t)(i * 32 + r0) * a.out_ld;
-            if (m0 + wm + i * 32 + r0 + lane / LPR >= a.m) continue;
-            if (n + EP <= a.n) {
-                put_bytes<false, sizeof o>(p, &o);
-            } else {
-#pragma unroll
-                for (int c = 0; c < EP; ++c)
-                    if (n + c < a.n) p[c] = o.v[c];
-            }
-        }
-        __builtin_amdgcn_wave_barrier();
+            multiply(set0, yes, stage, yes, step + 1 < end ? step + 1 : first, no, 0);
+            multiply(set1, yes, stage, no, 0, no, 0);
+            multiply(set2, yes, stage, no, 0, no, 0);
+            if (stored) landed(but_stores);
+            else landed(but_next);
+            stored = false;
+            multiply(set3, yes, after, no, 0, yes, stage);
+            fetched();
+            stage = after;
+        } while (++step < end);
+        store(m, n);
+        stored = true;
+        if (!more) break;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may come to LDS once it is another block's)
 }
 
 // The parts of a split sum added up in their order and rounded: four outputs per thread.
@@ -369,7 +426,10 @@ static hipError_t run_tiles(const Product4Args &a, const Scales4 &sx, const Scal
         return r != hipSuccess ? r : run_tiles<BM, BN, WM, WN, STAGES, TO, PARTIAL>(hi, hx, hw, splits, s);
     }
     const int32_t steps = (int32_t)steps_of(a.blocks), per = (steps + splits - 1) / splits;
-    const dim3 grid((unsigned)(tm * tn), (unsigned)((steps + per - 1) / per)), block(BM / WM * (BN / WN) * WAVE);
+    // As many blocks as run at a time, where each has several tiles.
+    constexpr int64_t AT_ONCE = CUS * (LDS_BYTES / (STAGES * (BM + BN) * KT));
+    const int64_t blocks = splits > 1 || tm * tn < AT_ONCE ? tm * tn : AT_ONCE;
+    const dim3 grid((unsigned)blocks, (unsigned)((steps + per - 1) / per)), block(BM / WM * (BN / WN) * WAVE);
     return launch(k_product4<BM, BN, WM, WN, STAGES, TO, PARTIAL>, grid, block, s, a, sx, sw, (int32_t)tn, (uint32_t)tm, per);
 }
 
@@ -386,7 +446,7 @@ static hipError_t run_cut(const Product4Args &a, const Scales4 &sx, const Scales
 hipError_t run_product4(const Product4Args &given, hipStream_t s)
 {
     Product4Args a = given;
-    if (a.m == 1) a.x_ld = a.xs_ld = 0;  // the stride of a single row is never used
+    if (a.m == 1) a.x_ld = a.xs_ld = a.out_ld = 0;  // the stride of a single row is never used
     if (a.n == 1) a.w_ld = a.ws_ld = 0;
     const Cut c = cut_product(a.m, a.n, (int64_t)a.blocks * CHUNK);
     Scales4 sx{a.xs, a.xs_ld, CPR}, sw{a.ws, a.ws_ld, CPR};

@@ -298,7 +298,7 @@ static sp_status check_rows4(const char *what, const void *q, const void *scales
 {
     if (!q || !scales) return bad("null %s", what);
     if (q_ld < blocks * 16 || (n > 1 && q_ld >= MAX_LD4)) return bad("row stride %lld of %s not in %lld..2^23", (long long)q_ld, what, (long long)blocks * 16);
-    if (scales_ld < blocks || scales_ld > MAX_LD) return bad("row stride %lld of the scales of %s not in %lld..2^40", (long long)scales_ld, what, (long long)blocks);
+    if (scales_ld < blocks || (n > 1 && scales_ld >= MAX_LD4)) return bad("row stride %lld of the scales of %s not in %lld..2^23", (long long)scales_ld, what, (long long)blocks);
     if (((uintptr_t)q | (uintptr_t)scales | (n > 1 ? (uint64_t)q_ld | (uint64_t)scales_ld : 0)) % 16 != 0)
         return bad("rows of %s and their scales are to start at multiples of 16 bytes", what);
     return SP_OK;
@@ -317,6 +317,7 @@ extern "C" sp_status sp_product4(const uint8_t *x, const uint8_t *x_scales, int6
     TRY(check_rows4("x", x, x_scales, m, blocks, x_ld, x_scales_ld));
     TRY(check_rows4("w", w, w_scales, n, blocks, w_ld, w_scales_ld));
     TRY(check_rows("output", out, out_type, m, n, out_ld));
+    if (m > 1 && out_ld >= MAX_LD4) return bad("row stride %lld of output not below 2^23", (long long)out_ld);
     TRY(check_workspace(workspace, workspace_bytes, need));
     const Product4Args a{x, x_scales, w, w_scales, m, n, (int32_t)blocks, x_ld, x_scales_ld, w_ld, w_scales_ld,
                          out, out_type, out_ld, (char *)workspace};

@@ -487,13 +487,13 @@ def _factor4(q, scales, what):
     n, width = q.shape
     (ld, step), (sld, sstep) = q.stride(), scales.stride()
     at, sat = q.data_ptr(), scales.data_ptr()
-    if (at | sat | ld | sld) % 16 == 0 and step == 1 and sstep == 1 and width <= ld < 1 << 23 and sld >= width // 16:
+    if (at | sat | ld | sld) % 16 == 0 and step == 1 and sstep == 1 and width <= ld < 1 << 23 and width // 16 <= sld < 1 << 23:
         return q, scales, at, ld, sat, sld
     given = []
-    for t, to, most in zip((q, scales), _strides4(2 * width), (1 << 23, 1 << 40)):
+    for t, to in zip((q, scales), _strides4(2 * width)):
         width = t.shape[1]
         if t.data_ptr() % 16 or (width > 1 and t.stride(1) != 1) or (
-                n > 1 and not (width <= t.stride(0) < most and t.stride(0) % 16 == 0)):
+                n > 1 and not (width <= t.stride(0) < 1 << 23 and t.stride(0) % 16 == 0)):
             t = torch.empty((n, to), dtype=torch.uint8, device=t.device)[:, :width].copy_(t)
         given.append((t, t.data_ptr(), t.stride(0) if n > 1 else to))
     (q, at, ld), (scales, sat, sld) = given

@@ -51,7 +51,9 @@ GRAD = dict(list(DISTILL.items())[:13] + [("weight", 1.0), ("weights", A), ("los
     ("sp_product4", PRODUCT4, dict(w_ld=32), "stride"),
     ("sp_product4", PRODUCT4, dict(w_ld=1 << 23), "stride"),
     ("sp_product4", PRODUCT4, dict(x_scales_ld=2), "stride"),
+    ("sp_product4", PRODUCT4, dict(w_scales_ld=1 << 23), "stride"),
     ("sp_product4", PRODUCT4, dict(out_ld=7), "stride"),
+    ("sp_product4", PRODUCT4, dict(out_ld=1 << 23), "stride"),
     ("sp_product4", PRODUCT4, dict(out_type=tk.SP_I8), "element type"),
     ("sp_adjust", ADJUST, dict(type=tk.SP_F8), "element type"),
     ("sp_adjust", ADJUST, dict(n=1 << 31), "rows"),
