@@ -366,7 +366,10 @@ __global__ void __launch_bounds__(BLOCK) k_product_join(ProductArgs a, int32_t s
 //   64 x 4096 x 4096                   25      18     14     13   11 (4 of 64x64)
 //   33 x 2000 x 512                     7       6      5      5    7 (2 of 32x64)
 //   424 x 222 x 3424          40       23      16     12     12    9 (4 of 32x64)
-Cut cut_product(int64_t m, int64_t n, int64_t k)
+struct Cut {
+    int32_t tile, splits;
+};
+static Cut cut_product(int64_t m, int64_t n, int64_t k)
 {
     constexpr struct {
         int bm, bn;

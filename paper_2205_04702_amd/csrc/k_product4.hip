@@ -392,14 +392,58 @@ __global__ void __launch_bounds__(BLOCK) k_pack_scales(const uint8_t *scales, in
 
 static int64_t steps_of(int32_t blocks) { return (blocks + CPR - 1) / CPR; }
 
-// Packed scales pay for themselves where many tiles read them.
-static bool packs(int64_t m, int64_t n, const Cut &c) { return c.tile == 0 && c.splits == 1; }
+// How a product is cut: into tiles, and parts of k where the tiles are few.  The estimate, in us, for
+// what a CU has to do one after the other: rounds of as many blocks as run at a time, each a fixed time
+// (first loads, outputs) and its steps of k, with a block on a CU or as many as fit; for tiles of 256
+// the packing of the scales; for parts a second launch and their traffic.  Measured on both sides
+// of the lines that it draws (us a call, of which 8.7 are the host's, in two launches 13; bf16):
+//                          256x256  128x128  64x128  64x64  32x64   in parts
+//   8192 x 16384 x 4096        302
+//   8192 x 8192 x 512           52       48      61     73     93
+//   4000 x 4000 x 4000          44       57      74     94    107
+//   4000 x 4000 x 1000          24       18      22     28     34
+//   777 x 10001 x 1000          32       18      17     19     21
+//   2048 x 2048 x 2048          26       11      12     14     18
+//   256 x 8192 x 8192           55       29      23     28     36   26 (2 of 128x128)
+//   128 x 8192 x 8192           54       29      22     18     19   19 (2 of 64x128)
+//   64 x 4096 x 4096            33       13      11      9      9   13 (2 of any)
+//   1 x 131072 x 2048           53       31      28     29     28   37 (2 of 64x128)
+//   1 x 4096 x 8192             53       22      19     16     15   13 (4 of 64x64)
+struct Cut {
+    int32_t tile, splits;
+};
+static Cut cut_product4(int64_t m, int64_t n, int32_t blocks)
+{
+    constexpr struct {
+        int bm, bn, at_once;
+        double alone, beside, fixed, once;
+    } T[] = {{256, 256, 256, 2.05, 2.15, 6.0, 8.0}, {128, 128, 512, 0.85, 1.6, 2.6, 0.0}, {64, 128, 512, 0.65, 1.05, 1.5, 0.0},
+             {64, 64, 512, 0.5, 0.75, 1.4, 0.0}, {32, 64, 768, 0.42, 0.57, 0.6, 0.0}};
+    const int64_t steps = steps_of(blocks);
+    Cut best{1, 1};
+    double least = 1e300;
+    for (int t = 0; t < 5; ++t) {
+        const double tiles = (double)((m + T[t].bm - 1) / T[t].bm) * (double)((n + T[t].bn - 1) / T[t].bn);
+        for (int sp = 1; sp <= 16; sp *= 2) {
+            if (sp > 1 && (t == 0 || steps < 4 * sp || tiles * sp > 1024)) break;
+            const double all = tiles * sp, step = all <= (double)CUS ? T[t].alone : T[t].beside;
+            double us = T[t].once + std::ceil(all / T[t].at_once) * (T[t].fixed + step * (double)((steps + sp - 1) / sp));
+            if (sp > 1) us += 4.5 + (double)m * (double)n * 4.0 * (2 * sp) / 4e6;
+            if (us < least) least = us, best = Cut{t, sp};
+        }
+    }
+    return best;
+}
+
+// The scales of tiles of 256 are packed: what each reads of them in the caller's rows is as many lines as
+// the factors' (8192^3: 324 us with both in the caller's rows, 272 packed, of which 5 for packing).
+static bool packs(const Cut &c) { return c.tile == 0; }
 
 int64_t product4_workspace(int64_t m, int64_t n, int32_t blocks)
 {
     if (m == 0 || n == 0) return 0;
-    const Cut c = cut_product(m, n, (int64_t)blocks * CHUNK);
-    return c.splits > 1 ? m * n * 4 * c.splits : packs(m, n, c) ? steps_of(blocks) * 8 * (m + n) : 0;
+    const Cut c = cut_product4(m, n, blocks);
+    return c.splits > 1 ? m * n * 4 * c.splits : packs(c) ? steps_of(blocks) * 8 * (m + n) : 0;
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool PARTIAL>
@@ -437,7 +481,7 @@ template <typename TO, bool PARTIAL>
 static hipError_t run_cut(const Product4Args &a, const Scales4 &sx, const Scales4 &sw, const Cut &c, hipStream_t s)
 {
     return c.tile == 0   ? run_tiles<256, 256, 128, 128, 2, TO, PARTIAL>(a, sx, sw, c.splits, s)
-           : c.tile == 1 ? run_tiles<128, 128, 64, 64, 4, TO, PARTIAL>(a, sx, sw, c.splits, s)
+           : c.tile == 1 ? run_tiles<128, 128, 64, 64, 2, TO, PARTIAL>(a, sx, sw, c.splits, s)
            : c.tile == 2 ? run_tiles<64, 128, 32, 64, 3, TO, PARTIAL>(a, sx, sw, c.splits, s)
            : c.tile == 3 ? run_tiles<64, 64, 32, 32, 4, TO, PARTIAL>(a, sx, sw, c.splits, s)
                          : run_tiles<32, 64, 32, 32, 4, TO, PARTIAL>(a, sx, sw, c.splits, s);
@@ -448,9 +492,9 @@ hipError_t run_product4(const Product4Args &given, hipStream_t s)
     Product4Args a = given;
     if (a.m == 1) a.x_ld = a.xs_ld = a.out_ld = 0;  // the stride of a single row is never used
     if (a.n == 1) a.w_ld = a.ws_ld = 0;
-    const Cut c = cut_product(a.m, a.n, (int64_t)a.blocks * CHUNK);
+    const Cut c = cut_product4(a.m, a.n, a.blocks);
     Scales4 sx{a.xs, a.xs_ld, CPR}, sw{a.ws, a.ws_ld, CPR};
-    if (packs(a.m, a.n, c)) {
+    if (packs(c)) {
         const auto pack = [&](Scales4 &side, int64_t rows, uint2 *to) {
             const dim3 grid((unsigned)((rows + 63) / 64), (unsigned)((steps_of(a.blocks) + 15) / 16));
             const hipError_t e = launch(k_pack_scales, grid, dim3(BLOCK), s, side.p, side.row, rows, a.blocks, to);

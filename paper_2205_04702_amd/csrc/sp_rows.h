@@ -627,10 +627,6 @@ struct ProductArgs {
     int64_t out_ld;
     char *work;
 };
-struct Cut {
-    int32_t tile, splits;
-};
-Cut cut_product(int64_t m, int64_t n, int64_t bytes);  // rows of so many bytes
 int64_t product_workspace(int64_t m, int64_t n, int64_t k);
 hipError_t run_product(const ProductArgs &a, hipStream_t s);
 
