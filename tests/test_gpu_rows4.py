@@ -130,6 +130,25 @@ def test_many_rows():
     assert torch.equal(got.cpu().double(), ref.values4(want_q, want_s)[:, :dim])
 
 
+@pytest.mark.parametrize("dim,lead,ld", [(1001, 0, 1001), (1001, 3, 1011), (1024, 0, 1024), (1024, 16, 1040), (1024, 5, 1029), (2000, 1, 2004),
+                                         (40, 0, 41), (7, 0, 7), (3, 1, 5), (16, 0, 16)])
+def test_many_rows_into_fp32(dim, lead, ld):
+    """The forms of large reads into fp32: rows that start at any place of a line, slots that are none."""
+    n, slots = (1 << 20) // ((dim + 7) // 8) + 77, 300
+    q, s = some_rows(slots, dim, dim, -130, 125)
+    s[::7] = 255
+    s[1::7] = 0
+    at = torch.randint(-1, slots + 1, (n,), generator=torch.Generator().manual_seed(9))
+    buf = torch.full((n * ld + lead + 8,), 9.0, device="cuda")
+    out = buf[lead:lead + n * ld].view(n, ld)[:, :dim]
+    got = tk.cache_read4(q, s, at.cuda(), dim, F32, out=out).cpu()
+    table = torch.cat([ref.values4(q.cpu(), s.cpu())[:, :dim].float(), torch.zeros((1, dim))])
+    want = table[torch.where((at < 0) | (at >= slots), slots, at)]
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+    out.fill_(9.0)
+    assert (buf == 9).all()
+
+
 # ------------------------------------------------------------------ products
 
 SHAPES = [(1, 1, 1), (1, 300, 32), (2, 5, 33), (3, 70, 100), (31, 33, 129), (33, 64, 512), (64, 200, 513), (65, 65, 640),
@@ -164,6 +183,42 @@ def test_product_lengths(k):
         whole = torch.as_strided(t, (t.shape[0], t.stride(0)), t.stride())
         whole[:, 16 * blocks:] = 0x77
     close4(tk.product4(x, xs, w, ws, F32), x, xs, w, ws, F32)
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [
+    (8100, 8001, 2000, BF16),    # tiles of 256, several for each block, rows that end inside a store
+    (8192, 8192, 2048, F32),     # ... whole ones
+    (4000, 4104, 4000, F16),     # ... one for each block
+    (8200, 8192, 300, F16),      # tiles of 128, several for each block
+    (8200, 8191, 256, F32),
+    (777, 10_001, 1000, BF16),   # tiles of 64 x 128
+    (128, 8192, 8192, F32),      # tiles of 64
+    (1, 70_000, 2048, BF16),     # tiles of 32 x 64
+    (31, 131_072, 32, BF16),
+    (1, 4096, 8192, F16),        # parts of k
+    (40, 50, 65_536, F32),
+    (3, 5, 1 << 20, F32),        # the longest rows
+])
+def test_large_products(m, n, k, dtype):
+    """Values that are small multiples of a half, with scales of 1 or a half: every sum is a multiple of 1 / 16 below
+    2^20, exact in fp32 in any order, so the product is the exact one, rounded once."""
+    g = torch.Generator(device="cuda").manual_seed(k)
+    sides = []
+    for rows in (m, n):
+        q, s = tk.empty_cache4(rows, k)
+        code = torch.randint(0, 4, (rows, q.shape[1] * 2), generator=g, device="cuda", dtype=torch.uint8)
+        code |= torch.randint(0, 2, code.shape, generator=g, device="cuda", dtype=torch.uint8) << 3
+        code[:, k:] = 0
+        q.copy_(code[:, 0::2] | code[:, 1::2] << 4)
+        s.copy_(torch.randint(126, 128, s.shape, generator=g, device="cuda", dtype=torch.uint8))
+        value = (code & 7).float() * 0.5
+        value = torch.where(code >= 8, -value, value) * torch.exp2(s.float() - 127).repeat_interleave(32, 1)
+        sides += [q, s, value]
+    x, xs, a, w, ws, b = sides
+    want = torch.zeros((m, n), device="cuda")
+    for i in range(0, a.shape[1], 8192):
+        want += a[:, i:i + 8192] @ b[:, i:i + 8192].t().contiguous()
+    assert torch.equal(tk.product4(x, xs, w, ws, dtype), want.to(dtype))
 
 
 def test_product_of_the_smallest_and_largest_scales():
