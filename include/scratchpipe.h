@@ -556,7 +556,8 @@ sp_status sp_adjust(const void *scores, int32_t type, int64_t n, int64_t vocab, 
  *
  * sp_distill_grad gives the loss and the gradient of weight * loss[i] to the scores,
  *     grad[i][v] = weight * T * (q_v - sum over j with token(j) = v of p_j),
- * zeros for a row of loss 0 by lack of entries.  weights [n] fp32: each row's in place of the number
+ * zeros for a row of loss 0 by lack of entries (a row's sums are taken in an order that goes by its
+ * sizes and by where its gradient starts in 64 bytes).  weights [n] fp32: each row's in place of the number
  * (NULL: the number).  grad: SP_F32, SP_BF16 or SP_F16; it may be scores itself (same pointer,
  * type and ld).
  * workspace: as for sp_lookup_grad, of the bytes that sp_distill_workspace gives for n, vocab, k and

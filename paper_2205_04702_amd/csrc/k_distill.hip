@@ -216,7 +216,12 @@ __device__ __forceinline__ Soft wave_soft(Soft s, float c)
 // the sums, and after the teacher's entries were noted: a bit for each column of the held units, and a
 // hash from token to entry, so that a unit is stored once, with its corrections (stored over
 // the gradient afterwards, they cost 58 of 181 us at 20000 x 8192 in bf16 with 64 entries).
-template <typename T, typename TO, int NT, int HELD, bool GRAD, bool STREAM>
+//
+// Units are counted from where 64 aligned bytes of the gradient's row start, and the columns before (head) and
+// behind them (rest) go one by one, so that the gradient may go past the caches wherever rows start: parts
+// of 64 bytes that two waves write there cost a read each, and through the caches 8192 x 50001 in
+// bf16 took 385 us, 340 so.
+template <typename T, typename TO, int NT, int HELD, bool GRAD>
 __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(DistillArgs a)
 {
     constexpr int N = 4, C = COLS<T>, NW = NT / WAVE;  // N units are added at once
@@ -231,8 +236,23 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
     int t = (int)threadIdx.x;
     const int wave = wave_id(), entry_waves = (a.k + WAVE - 1) / WAVE, mask = hash_mask(a.k);
     const float c = LOG2E / a.temperature;
-    const int32_t units = a.vocab / C, rest = a.vocab - units * C;
-    const auto scores_of = [&](int64_t row) { return (const T *)a.scores + row * a.ld; };
+    constexpr int LINE = 64 / (int)sizeof(TO);
+    struct Row {
+        const T *scores;
+        int32_t head, units, odd;  // columns before the units, units, columns that are in none
+        __device__ __forceinline__ int32_t odd_column(int t) const { return t < head ? t : units * C + t; }
+        __device__ __forceinline__ __amdgpu_buffer_rsrc_t from(bool on) const { return buffer(scores + head, on ? units * 16 : 0); }
+    };
+    const auto row_at = [&](int64_t row) {
+        Row r;
+        r.scores = (const T *)a.scores + row * a.ld;
+        r.head = GRAD ? (int32_t)(-((uintptr_t)((const TO *)a.grad + row * a.grad_ld) / sizeof(TO)) % LINE) : 0;
+        if (r.head > a.vocab) r.head = a.vocab;
+        r.units = (a.vocab - r.head) / C;
+        r.odd = a.vocab - r.units * C;
+        return r;
+    };
+    static_assert(LINE + C <= WAVE, "a thread for each odd column");
     // Whether any entry of a row counts, from what each wave found; a barrier lies between.
     const auto note_alive = [&](int turn, const Entry &e) {
         const bool on = __any(!(e.logit == NONE));
@@ -245,8 +265,9 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
     };
 
     unit r[HELD];
-    T last = from_float<T>(0.f);  // a column behind the last unit
+    T odd = from_float<T>(0.f);  // a column that is in no unit
     int64_t row = blockIdx.x;
+    Row here = row_at(row);
     RawEntry raw{};
     load_entry(a, row, raw);
     Entry e = entry_of(a, raw);
@@ -258,17 +279,17 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
     }
     __syncthreads();
     bool on = is_alive(1);
-    load_score(e, scores_of(row), raw);
-    if (t < rest) last = scores_of(row)[units * C + t];
+    load_score(e, here.scores, raw);
+    if (t < here.odd) odd = here.scores[here.odd_column(t)];
     {
-        const __amdgpu_buffer_rsrc_t from = buffer(scores_of(row), on ? units * 16 : 0);
+        const __amdgpu_buffer_rsrc_t from = here.from(on);
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) r[i] = load_unit<STREAM>(from, t + i * NT);
+        for (int i = 0; i < HELD; ++i) r[i] = load_unit<true>(from, t + i * NT);
     }
     for (int turn = 0;; turn ^= 1) {
         // (else every unit's place is worked out before the loop and kept)
         asm volatile("" : "+v"(t));
-        const T *scores = scores_of(row);
+        const int32_t units = here.units;
         const bool more = row + gridDim.x < a.n;
         const int64_t next = more ? row + gridDim.x : row;
         RawEntry raw_next{};
@@ -286,18 +307,18 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
                     add_units<T, N>(s, r + i, c);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-            const __amdgpu_buffer_rsrc_t from = buffer(scores, units * 16);
+            const __amdgpu_buffer_rsrc_t from = here.from(true);
             for (int32_t u = HELD * NT + t; u < units; u += N * NT) {
                 unit x[N];
 #pragma unroll
-                for (int k = 0; k < N; ++k) x[k] = load_unit<false>(from, u + k * NT);
+                for (int k = 0; k < N; ++k) x[k] = load_unit<!GRAD>(from, u + k * NT);
 #pragma unroll
                 for (int k = 0; k < N; ++k)
                     if (u + k * NT >= units) x[k] = all_of<T>(NONE);
                 add_units<T, N>(s, x, c);
             }
-            if (t < rest) {
-                const float v = to_float(last);
+            if (t < here.odd) {
+                const float v = to_float(odd);
                 join(s, Soft{v, v > NONE ? 1.f : v != v ? v : 0.f}, c);
             }
             s = wave_soft(s, c);
@@ -311,11 +332,12 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
         note_alive(turn, f);
         __syncthreads();
         const bool next_on = more && is_alive(turn);
-        const __amdgpu_buffer_rsrc_t from = buffer(scores_of(next), next_on ? units * 16 : 0);
-        const T own = last;
+        const Row coming = row_at(next);
+        const __amdgpu_buffer_rsrc_t from = coming.from(next_on);
+        const T own = odd;
         if (next_on) {
-            load_score(f, scores_of(next), raw_next);
-            if (t < rest) last = scores_of(next)[units * C + t];
+            load_score(f, coming.scores, raw_next);
+            if (t < coming.odd) odd = coming.scores[coming.odd_column(t)];
         }
         Soft m{NONE, 0.f};
         float p = 0.f;
@@ -334,9 +356,9 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
                     ps[t] = p;
                     if (e.token >= 0) {
                         note(hash[turn], mask, e.token, t);
-                        const int32_t u = e.token / C, i = u / NT;
-                        if (u < units && i < HELD)
-                            atomicOr(&columns[u % NT * (HELD / 4) + i / 4], 1u << (i % 4 * 8 + e.token % C));
+                        const int32_t v = e.token - here.head, u = v / C, i = u / NT;
+                        if (v >= 0 && u < units && i < HELD)
+                            atomicOr(&columns[u % NT * (HELD / 4) + i / 4], 1u << (i % 4 * 8 + v % C));
                     }
                 }
             }
@@ -344,7 +366,7 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
         if (GRAD) {
             clear(hash[turn ^ 1], mask);
             TO *grad = (TO *)a.grad + row * a.grad_ld;
-            const __amdgpu_buffer_rsrc_t to = buffer(grad, units * C * (int)sizeof(TO));
+            const __amdgpu_buffer_rsrc_t to = buffer(grad + here.head, units * C * (int)sizeof(TO));
             const float g = raw.weight * a.temperature;
             const float base = s.top > NONE ? s.top : 0.f, part = !on || s.sum == 0.f ? 0.f : 1.f / s.sum, by = part * g;
             __syncthreads();
@@ -363,36 +385,36 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
                 for (int k = 0; k < C; ++k) v[k] = on ? part_of(column<T>(x, k), base, c) * by : 0.f;
                 while (bits) {
                     const int at = __ffs(bits) - 1;
-                    const float by_teacher = corrected(u * C + at);
+                    const float by_teacher = corrected(here.head + u * C + at);
 #pragma unroll
                     for (int k = 0; k < C; ++k) v[k] -= k == at ? by_teacher : 0.f;
                     bits &= bits - 1;
                 }
-                store_unit<STREAM, TO>(to, u, v);
+                store_unit<true, TO>(to, u, v);
             };
 #pragma unroll
             for (int i = 0; i < HELD; ++i) {
                 store(r[i], t + i * NT, mine[i / 4] >> (i % 4 * 8) & 0xFF);
-                r[i] = load_unit<STREAM>(from, t + i * NT);
+                r[i] = load_unit<true>(from, t + i * NT);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (t < rest) {
-                const int32_t at = units * C + t;
+            if (t < here.odd) {
+                const int32_t at = here.odd_column(t);
                 float v = on ? part_of(to_float(own), base, c) * by : 0.f;
                 if (on && is_listed(hash[turn], mask, at)) v -= corrected(at);
                 grad[at] = from_float<TO>(v);
             }
             if (units > HELD * NT) {  // the same for all: what was not held, corrected afterwards
-                const __amdgpu_buffer_rsrc_t again = buffer(scores, on ? units * 16 : 0);
-                for (int32_t u = HELD * NT + t; u < units; u += NT) store(load_unit<STREAM>(again, u), u, 0);
+                const __amdgpu_buffer_rsrc_t again = here.from(on);
+                for (int32_t u = HELD * NT + t; u < units; u += NT) store(load_unit<true>(again, u), u, 0);
                 __syncthreads();
-                const int32_t u = e.token / C;
-                if (on && e.token >= 0 && u < units && u >= HELD * NT && is_first(hash[turn], mask, e.token, t))
+                const int32_t v = e.token - here.head;
+                if (on && e.token >= 0 && v / C >= HELD * NT && v < units * C && is_first(hash[turn], mask, e.token, t))
                     grad[e.token] = from_float<TO>(part_of(e.score, base, c) * by - corrected(e.token));
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < HELD; ++i) r[i] = load_unit<STREAM>(from, t + i * NT);
+            for (int i = 0; i < HELD; ++i) r[i] = load_unit<true>(from, t + i * NT);
             __syncthreads();
         }
         if (t == 0) {
@@ -403,6 +425,7 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
         }
         if (!more) return;
         row = next;
+        here = coming;
         e = f;
         raw = raw_next;
         on = next_on;
@@ -584,19 +607,15 @@ hipError_t run_distill(const DistillArgs &given, hipStream_t s)
                 return given.k <= 256 ? launch(k_distill_rest<T, TO, 256, true>, grid, dim3(256), s, given, q)
                                       : launch(k_distill_rest<T, TO, 1024, true>, grid, dim3(1024), s, given, q);
             }
-            const auto pick = [&](auto stream) {
-                constexpr bool S = decltype(stream)::value;
-                if (given.k <= 64 && units <= 64 * 4) return go(k_distill<T, TO, 64, 4, true, S>, 64, 20);
-                if (given.k <= 64 && units <= 64 * 16) return go(k_distill<T, TO, 64, 16, true, S>, 64, 16);
-                if (given.k <= 256 && units <= 256 * 4) return go(k_distill<T, TO, 256, 4, true, S>, 256, 20);
-                if (given.k <= 256 && units <= 256 * 16) return go(k_distill<T, TO, 256, 16, true, S>, 256, 16);
-                if (given.k <= 512 && units <= 512 * 16) return go(k_distill<T, TO, 512, 16, true, S>, 512, 16);
-                return go(k_distill<T, TO, 1024, 16, true, S>, 1024, 16);
-            };
             if (!given.grad)
-                return given.k <= 256 ? go(k_distill<T, float, 256, 4, false, true>, 256, 0)
-                                      : go(k_distill<T, float, 1024, 4, false, true>, 1024, 0);
-            return whole_pieces((const TO *)given.grad, given.grad_ld) ? pick(std::true_type()) : pick(std::false_type());
+                return given.k <= 256 ? go(k_distill<T, float, 256, 4, false>, 256, 0)
+                                      : go(k_distill<T, float, 1024, 4, false>, 1024, 0);
+            if (given.k <= 64 && units <= 64 * 4) return go(k_distill<T, TO, 64, 4, true>, 64, 20);
+            if (given.k <= 64 && units <= 64 * 16) return go(k_distill<T, TO, 64, 16, true>, 64, 16);
+            if (given.k <= 256 && units <= 256 * 4) return go(k_distill<T, TO, 256, 4, true>, 256, 20);
+            if (given.k <= 256 && units <= 256 * 16) return go(k_distill<T, TO, 256, 16, true>, 256, 16);
+            if (given.k <= 512 && units <= 512 * 16) return go(k_distill<T, TO, 512, 16, true>, 512, 16);
+            return go(k_distill<T, TO, 1024, 16, true>, 1024, 16);
         });
     });
 }

@@ -303,9 +303,30 @@ def test_distill_in_place_with_strides_and_dimensions(n, vocab):
     x.copy_(s)
     wide = torch.stack([tok, tok], 2).cuda()[None, :, :, 0]
     loss, grad = tk.distill_grad(x, wide, t.cuda()[None], 0.25, 2.0, out=x)
-    assert grad is x and torch.equal(x[0], want[1]) and torch.equal(loss[0], want[0])
+    # (Not the same bits as above: a row's sums are taken in units that start where 64 aligned bytes of the
+    # gradient do, so in another order; both are within what any order may be off.)
+    assert grad is x
+    check_distill(s, tok, t, torch.full((n,), 0.25), 2.0, loss[0], x[0], BF16)
+    x.copy_(s)
+    again = tk.distill_grad(x, wide, t.cuda()[None], 0.25, 2.0)
     x.fill_(6.0)
     assert (buf == 6).all()
+    check_distill(s, tok, t, torch.full((n,), 0.25), 2.0, again[0][0], again[1][0], BF16)
+
+
+@pytest.mark.parametrize("vocab", [5, 40, 129, 1001])
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (F32, F32), (F32, BF16), (F16, F32)])
+def test_distill_gradient_that_starts_anywhere(vocab, dtype, out):
+    """Every place of a gradient's row in its 64 bytes, with teacher's columns before, in and behind the units."""
+    k = min(vocab, 30)
+    s, tok, t, w = lesson(34, vocab, k, dtype, F32, 17)
+    for start in (0, 1, 2, 5, 31):
+        buf = torch.full((34 * (vocab + 1) + 40,), 6.0, dtype=out, device="cuda")
+        x = torch.as_strided(buf, (34, vocab), (vocab + 1, 1), start)
+        loss, grad = tk.distill_grad(s.cuda(), tok.cuda(), t.cuda(), w.cuda(), out=x)
+        check_distill(s, tok, t, w, 1.0, loss, grad, out)
+        x.fill_(6.0)
+        assert (buf == 6).all()
 
 
 def test_distill_gradient_against_differences():
