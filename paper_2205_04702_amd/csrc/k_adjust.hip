@@ -37,7 +37,7 @@ struct Tokens {
     {
 #pragma unroll
         for (int k = 0; k < N; ++k)
-            if (from + k * NT < n && v[k] >= first && v[k] < first + width) go((int32_t)v[k] - first, from + k * NT);
+            if (from + k * NT < n && (uint64_t)(v[k] - first) < (uint64_t)width) go((int32_t)(v[k] - first), from + k * NT);
     }
 };
 template <int NT, int N, class F>

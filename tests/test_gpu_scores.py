@@ -157,6 +157,20 @@ def test_adjust_in_place_and_twice(vocab):
     assert torch.equal(adjusted(r, numbers), want)
 
 
+@pytest.mark.parametrize("vocab", [3, 33, 200, 5001])
+@pytest.mark.parametrize("dtype", [F32, F16])
+def test_adjust_into_rows_that_start_anywhere(vocab, dtype):
+    """Every place of an output's row in its 64 bytes; columns before, in and behind the units."""
+    n, numbers = 33, (1.5, 0.25, 0.125)
+    r = request(n, vocab, 40, 9, True, True, dtype, 8)
+    for start in (0, 1, 7, 30):
+        buf = torch.full((n * (vocab + 1) + 40,), 4.0, dtype=dtype, device="cuda")
+        x = torch.as_strided(buf, (n, vocab), (vocab + 1, 1), start)
+        check_adjust(r, numbers, adjusted(r, numbers, out=x), dtype)
+        x.fill_(4.0)
+        assert (buf == 4).all()
+
+
 def test_adjust_one_token_all_the_time():
     """A text of one token, and rows that differ in nothing but their text's length."""
     n, vocab, length = 4, 3000, 20_000
