@@ -66,6 +66,8 @@ constexpr int32_t FREE = -1;
 template <int K>
 struct Hash {
     int32_t key[2 * K], first[2 * K], last[2 * K];
+    float p[2 * K];    // of all entries that list the token
+    int32_t repeated;  // some token is listed more than once
 };
 __device__ __forceinline__ int hash_of(int32_t token, int mask) { return (int)((uint32_t)token * 0x9E3779B1u >> 16) & mask; }
 __device__ __forceinline__ int hash_mask(int k)  // at most half of the slots are taken
@@ -78,29 +80,28 @@ template <int K>
 __device__ __forceinline__ void clear(Hash<K> &h, int mask)
 {
     for (int i = (int)threadIdx.x; i <= mask; i += (int)blockDim.x) h.key[i] = FREE, h.first[i] = K, h.last[i] = -1;
+    if (threadIdx.x == 0) h.repeated = 0;
 }
 template <int K>
-__device__ __forceinline__ void note(Hash<K> &h, int mask, int32_t token, int j)
+__device__ __forceinline__ void note(Hash<K> &h, int mask, int32_t token, int j, float p)
 {
     int at = hash_of(token, mask);
     for (;;) {
         const int32_t old = atomicCAS(&h.key[at], FREE, token);
+        if (old == token) h.repeated = 1;
         if (old == FREE || old == token) break;
         at = (at + 1) & mask;
     }
     atomicMin(&h.first[at], j);
     atomicMax(&h.last[at], j);
+    h.p[at] = p;  // (of repeated tokens add_repeated() takes care)
 }
-// The p of all entries that list a token, one of which does, in their order.
 template <int K>
-__device__ __forceinline__ float listed(const Hash<K> &h, int mask, int32_t token, const int32_t *tokens, const float *ps)
+__device__ __forceinline__ int slot_of(const Hash<K> &h, int mask, int32_t token)  // of a token that is there
 {
     int at = hash_of(token, mask);
     while (h.key[at] != token) at = (at + 1) & mask;
-    const int first = h.first[at], last = h.last[at];
-    float p = ps[first];
-    for (int i = first + 1; i <= last; ++i) p += tokens[i] == token ? ps[i] : 0.f;
-    return p;
+    return at;
 }
 template <int K>
 __device__ __forceinline__ bool is_listed(const Hash<K> &h, int mask, int32_t token)
@@ -109,12 +110,31 @@ __device__ __forceinline__ bool is_listed(const Hash<K> &h, int mask, int32_t to
     while (h.key[at] != token && h.key[at] != FREE) at = (at + 1) & mask;
     return h.key[at] == token;
 }
+
+// The sums of p of tokens that are listed more than once, as integers: p times the power of two that puts
+// the token's largest p between 2^50 and 2^51, so that no order of the additions changes them.  (Added up
+// entry after entry, each time from LDS, 8192 x 1500 with 512 random entries took 2.3 ms, 0.17 so.)
 template <int K>
-__device__ __forceinline__ bool is_first(const Hash<K> &h, int mask, int32_t token, int j)
+struct Repeats {
+    uint32_t top[2 * K];  // the largest p's bits
+    uint64_t sum[2 * K];
+};
+// Every thread of the block, if any token is repeated: entry threadIdx.x (token -1: none) and its p.
+template <int K>
+__device__ __forceinline__ void add_repeated(Repeats<K> &r, Hash<K> &h, int mask, int32_t token, float p)
 {
-    int at = hash_of(token, mask);
-    while (h.key[at] != token) at = (at + 1) & mask;
-    return h.first[at] == j;
+    for (int i = (int)threadIdx.x; i <= mask; i += (int)blockDim.x) r.top[i] = 0, r.sum[i] = 0;
+    __syncthreads();
+    const int slot = token >= 0 ? slot_of(h, mask, token) : 0;
+    const bool again = token >= 0 && h.first[slot] != h.last[slot];
+    if (again) atomicMax(&r.top[slot], __float_as_uint(p));
+    __syncthreads();
+    const int e = again ? (int)(r.top[slot] >> 23) : 0;
+    if (again) atomicAdd((unsigned long long *)&r.sum[slot], (unsigned long long)ldexpf(p, 177 - e));
+    __syncthreads();
+    if (again && h.first[slot] == (int)threadIdx.x)
+        h.p[slot] = e == 255 ? __uint_as_float(0x7FC00000u) : ldexpf((float)r.sum[slot], e - 177);
+    __syncthreads();
 }
 
 // ---------------------------------------------------------------- entries
@@ -230,8 +250,7 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
     __shared__ float losses[NW];
     __shared__ int32_t alive[2][NW];
     __shared__ Hash<NT> hash[2];
-    __shared__ int32_t tokens[NT];
-    __shared__ float ps[NT];
+    __shared__ Repeats<NT> repeats;
     __shared__ uint32_t columns[GRAD ? NT * HELD / 4 : 1];  // a byte for each held unit, a thread's together
     int t = (int)threadIdx.x;
     const int wave = wave_id(), entry_waves = (a.k + WAVE - 1) / WAVE, mask = hash_mask(a.k);
@@ -352,10 +371,8 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
                 const float loss = wave_total(loss_of(e, p, m, s, a.temperature));
                 if (lane_id() == 0) losses[wave] = loss;
                 if (GRAD) {
-                    tokens[t] = e.token;
-                    ps[t] = p;
                     if (e.token >= 0) {
-                        note(hash[turn], mask, e.token, t);
+                        note(hash[turn], mask, e.token, t, p);
                         const int32_t v = e.token - here.head, u = v / C, i = u / NT;
                         if (v >= 0 && u < units && i < HELD)
                             atomicOr(&columns[u % NT * (HELD / 4) + i / 4], 1u << (i % 4 * 8 + v % C));
@@ -376,7 +393,9 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
                 mine[i] = columns[t * (HELD / 4) + i];
                 columns[t * (HELD / 4) + i] = 0;
             }
-            const auto corrected = [&](int32_t token) { return listed(hash[turn], mask, token, tokens, ps) * g; };
+            if (hash[turn].repeated)  // the same for all
+                add_repeated(repeats, hash[turn], mask, e.token, p);
+            const auto corrected = [&](int32_t token) { return hash[turn].p[slot_of(hash[turn], mask, token)] * g; };
             const auto store = [&](unit x, int32_t u, uint32_t bits) {
                 float v[C];
                 // (converted again: else the sums' fp32 values are kept in registers till here)
@@ -409,7 +428,7 @@ __global__ void __launch_bounds__(NT, HELD > 4 || NT > 512 ? 4 : 5) k_distill(Di
                 for (int32_t u = HELD * NT + t; u < units; u += NT) store(load_unit<true>(again, u), u, 0);
                 __syncthreads();
                 const int32_t v = e.token - here.head;
-                if (on && e.token >= 0 && v / C >= HELD * NT && v < units * C && is_first(hash[turn], mask, e.token, t))
+                if (on && e.token >= 0 && v / C >= HELD * NT && v < units * C && hash[turn].first[slot_of(hash[turn], mask, e.token)] == t)
                     grad[e.token] = from_float<TO>(part_of(e.score, base, c) * by - corrected(e.token));
             }
         } else {
@@ -504,8 +523,7 @@ __global__ void __launch_bounds__(NT) k_distill_rest(DistillArgs a, Parts q)
     __shared__ Soft masses[NW];
     __shared__ float losses[NW];
     __shared__ Hash<NT> hash;
-    __shared__ int32_t tokens[NT];
-    __shared__ float ps[NT];
+    __shared__ Repeats<NT> repeats;
     const int64_t row = blockIdx.y;
     const int part = (int)blockIdx.x, t = (int)threadIdx.x, wave = wave_id();
     const int entry_waves = (a.k + WAVE - 1) / WAVE, mask = hash_mask(a.k);
@@ -538,9 +556,7 @@ __global__ void __launch_bounds__(NT) k_distill_rest(DistillArgs a, Parts q)
         const float loss = wave_total(loss_of(e, p, m, s, a.temperature));
         if (lane_id() == 0) losses[wave] = loss;
         if (GRAD) {
-            tokens[t] = e.token;
-            ps[t] = p;
-            if (e.token >= 0) note(hash, mask, e.token, t);
+            if (e.token >= 0) note(hash, mask, e.token, t, p);
         }
     }
     if (GRAD) {
@@ -564,9 +580,10 @@ __global__ void __launch_bounds__(NT) k_distill_rest(DistillArgs a, Parts q)
         if (own_rest && t < rest)
             grad[units * C + t] = from_float<TO>(on ? part_of(to_float(scores[units * C + t]), base, c) * by : 0.f);
         __syncthreads();  // the teacher's columns again, over what was stored
+        if (hash.repeated) add_repeated(repeats, hash, mask, on ? e.token : -1, p);  // the same for all
         if (on && e.token >= 0 && ((e.token >= first * C && e.token < end * C) || (own_rest && e.token >= units * C)) &&
-            is_first(hash, mask, e.token, t))
-            grad[e.token] = from_float<TO>(part_of(e.score, base, c) * by - listed(hash, mask, e.token, tokens, ps) * g);
+            hash.first[slot_of(hash, mask, e.token)] == t)
+            grad[e.token] = from_float<TO>(part_of(e.score, base, c) * by - hash.p[slot_of(hash, mask, e.token)] * g);
     } else {
         __syncthreads();
     }
@@ -607,13 +624,16 @@ hipError_t run_distill(const DistillArgs &given, hipStream_t s)
                 return given.k <= 256 ? launch(k_distill_rest<T, TO, 256, true>, grid, dim3(256), s, given, q)
                                       : launch(k_distill_rest<T, TO, 1024, true>, grid, dim3(1024), s, given, q);
             }
-            if (!given.grad)
-                return given.k <= 256 ? go(k_distill<T, float, 256, 4, false>, 256, 0)
-                                      : go(k_distill<T, float, 1024, 4, false>, 1024, 0);
+            if (!given.grad) {
+                if (given.k <= 64 && units <= 64 * 8) return go(k_distill<T, float, 64, 4, false>, 64, 0);
+                if (given.k <= 256 && (given.n > CUS || units <= 1024)) return go(k_distill<T, float, 256, 4, false>, 256, 0);
+                return go(k_distill<T, float, 1024, 4, false>, 1024, 0);
+            }
             if (given.k <= 64 && units <= 64 * 4) return go(k_distill<T, TO, 64, 4, true>, 64, 20);
             if (given.k <= 64 && units <= 64 * 16) return go(k_distill<T, TO, 64, 16, true>, 64, 16);
             if (given.k <= 256 && units <= 256 * 4) return go(k_distill<T, TO, 256, 4, true>, 256, 20);
             if (given.k <= 256 && units <= 256 * 16) return go(k_distill<T, TO, 256, 16, true>, 256, 16);
+            if (given.k <= 512 && units <= 512 * 4) return go(k_distill<T, TO, 512, 4, true>, 512, 16);
             if (given.k <= 512 && units <= 512 * 16) return go(k_distill<T, TO, 512, 16, true>, 512, 16);
             return go(k_distill<T, TO, 1024, 16, true>, 1024, 16);
         });
