@@ -150,7 +150,7 @@ hipError_t run_adjust(const AdjustArgs &a, hipStream_t s)
         using T = decltype(t);
         const auto go = [&](auto kern, int nt, int u) {
             const int64_t width = (int64_t)u * nt * COLS<T>, stretches = (a.vocab + width - 1) / width;
-            const int64_t each = LAUNCH_BLOCKS / 2 / stretches;
+            const int64_t each = LAUNCH_BLOCKS / 4 / stretches;  // (of up to 1024 threads)
             for (int64_t i = 0; i < a.n; i += each) {
                 AdjustArgs p = a;
                 p.n = a.n - i < each ? a.n - i : each;

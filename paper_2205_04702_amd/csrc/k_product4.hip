@@ -49,6 +49,11 @@ struct Scales4 {
 // lane's scales, eight bytes of its row, come to registers a step ahead, and one byte permutation leaves
 // those of its half, a byte for each set.  w is the left factor of the matrix instruction: its four
 // consecutive rows per lane are four consecutive outputs.
+//
+// 8192^3 272 us, 4.0 PFLOP/s, 8192 x 16384 x 4096 302; matrix instructions alone, on registers of random
+// codes, reach 6.1 PFLOP/s at the clock that power leaves (8.7 on zeros).  256 x 256 in four waves of
+// 128 x 128 and not eight of 128 x 64: with those LDS was read for as long as the matrix cores were
+// busy (517 us with steps of 64 bytes and the scales through LDS; without scales 326, without loads 328).
 template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool PARTIAL>
 __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
     k_product4(Product4Args a, Scales4 sx, Scales4 sw, int32_t tiles_n, uint32_t tiles_m, int32_t per_split)
@@ -437,13 +442,14 @@ static Cut cut_product4(int64_t m, int64_t n, int32_t blocks)
 
 // The scales of tiles of 256 are packed: what each reads of them in the caller's rows is as many lines as
 // the factors' (8192^3: 324 us with both in the caller's rows, 272 packed, of which 5 for packing).
-static bool packs(const Cut &c) { return c.tile == 0; }
+// (In one launch: of fewer than 2^30 rows.)
+static bool packs(int64_t m, int64_t n, const Cut &c) { return c.tile == 0 && m < 1 << 30 && n < 1 << 30; }
 
 int64_t product4_workspace(int64_t m, int64_t n, int32_t blocks)
 {
     if (m == 0 || n == 0) return 0;
     const Cut c = cut_product4(m, n, blocks);
-    return c.splits > 1 ? m * n * 4 * c.splits : packs(c) ? steps_of(blocks) * 8 * (m + n) : 0;
+    return c.splits > 1 ? m * n * 4 * c.splits : packs(m, n, c) ? steps_of(blocks) * 8 * (m + n) : 0;
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool PARTIAL>
@@ -494,7 +500,7 @@ hipError_t run_product4(const Product4Args &given, hipStream_t s)
     if (a.n == 1) a.w_ld = a.ws_ld = 0;
     const Cut c = cut_product4(a.m, a.n, a.blocks);
     Scales4 sx{a.xs, a.xs_ld, CPR}, sw{a.ws, a.ws_ld, CPR};
-    if (packs(c)) {
+    if (packs(a.m, a.n, c)) {
         const auto pack = [&](Scales4 &side, int64_t rows, uint2 *to) {
             const dim3 grid((unsigned)((rows + 63) / 64), (unsigned)((steps_of(a.blocks) + 15) / 16));
             const hipError_t e = launch(k_pack_scales, grid, dim3(BLOCK), s, side.p, side.row, rows, a.blocks, to);

@@ -382,7 +382,7 @@ static sp_status check_distill(const void *scores, int32_t type, int64_t n, int6
     if (!is_float(type) || !is_float(teacher_type)) return bad("element type of the scores or the teacher");
     if (!is_index(token_type)) return bad("token type %d", token_type);
     TRY(sp_distill_workspace(n, vocab, k, grad, &need));
-    if (!(temperature > 0.f && std::isfinite(temperature) && std::isfinite(1.f / temperature)))
+    if (!(temperature > 0.f && std::isfinite(temperature) && std::isfinite(2.f / temperature)))  // (log2(e) / temperature is a number)
         return bad("temperature %g is no positive number", (double)temperature);
     TRY(check_rows("scores", scores, type, n, vocab, ld));
     TRY(check_rows("tokens", tokens, token_type, n, k, tokens_ld));

@@ -205,3 +205,27 @@ def test_long_lists_and_rows_past_32_bits():
     assert not tk.cache_read4(q, sc, at[1:] - 1).any()
     scores = tk.product4(*tk.quantize4(x[:1]), q, sc, F32)
     assert scores.shape == (1, 9_000_000) and (scores[0, at] == 1024 * 2.25).all() and int(torch.count_nonzero(scores)) == 3
+
+
+def test_more_rows_than_one_launch_has_blocks():
+    """Calls of 2^22 blocks and more of 1024 threads, and of a block for each of as many rows."""
+    n, vocab = (1 << 22) + 3, 2
+    s = torch.zeros((n, vocab), dtype=BF16, device="cuda")
+    s[:, 1] = 2.0
+    previous = torch.cat([torch.ones(3, dtype=torch.int64), torch.full((8200,), -1)]).cuda()  # for all rows
+    got = tk.adjust(s, previous, 2.0, 0.25, 0.125)
+    assert not got[:, 0].any() and (got[:, 1] == 2.0 / 2 - 0.25 - 3 * 0.125).all()
+    tok, t = torch.ones((n, 1), dtype=torch.int32, device="cuda"), torch.zeros((n, 1), device="cuda")
+    loss = tk.distill(s, tok, t)
+    again, grad = tk.distill_grad(s, tok, t)
+    want, want_grad, off, grad_off = ref.distill(s[:1].cpu(), tok[:1].cpu(), t[:1].cpu(), torch.ones(1), 1.0)
+    for one in (loss, again):
+        assert (one == one[0]).all() and (one[0].cpu().double() - want[0]).abs() <= off[0] + want[0].abs() * UNIT[F32]
+    assert (grad == grad[0]).all()
+    assert ((grad[0].cpu().double() - want_grad[0]).abs() <= grad_off[0] + (want_grad[0].abs() + grad_off[0]) * UNIT[BF16] + TINY[BF16]).all()
+
+
+def test_lists_of_no_width():
+    s = torch.randn((2, 3, 40), device="cuda")
+    none = torch.empty((2, 3, 0), dtype=torch.int64, device="cuda")
+    assert torch.equal(tk.adjust(s, none, bias_tokens=none, bias=none.float()), s)

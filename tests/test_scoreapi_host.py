@@ -87,6 +87,7 @@ GRAD = dict(list(DISTILL.items())[:13] + [("weight", 1.0), ("weights", A), ("los
     ("sp_distill", DISTILL, dict(temperature=0.0), "temperature"),
     ("sp_distill", DISTILL, dict(temperature=-1.0), "temperature"),
     ("sp_distill", DISTILL, dict(temperature=1e-45), "temperature"),
+    ("sp_distill", DISTILL, dict(temperature=4e-39), "temperature"),
     ("sp_distill", DISTILL, dict(temperature=NAN), "temperature"),
     ("sp_distill", DISTILL, dict(tokens_ld=4), "stride"),
     ("sp_distill", DISTILL, dict(loss=0), "null loss"),
