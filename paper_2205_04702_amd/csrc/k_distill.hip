@@ -130,10 +130,10 @@ __device__ __forceinline__ void add_repeated(Repeats<K> &r, Hash<K> &h, int mask
     if (again) atomicMax(&r.top[slot], __float_as_uint(p));
     __syncthreads();
     const int e = again ? (int)(r.top[slot] >> 23) : 0;
-    if (again) atomicAdd((unsigned long long *)&r.sum[slot], (unsigned long long)ldexpf(p, 177 - e));
+    if (again) atomicAdd((unsigned long long *)&r.sum[slot], e < 255 ? (unsigned long long)ldexpf(p, 177 - e) : 0ull);
     __syncthreads();
-    if (again && h.first[slot] == (int)threadIdx.x)
-        h.p[slot] = e == 255 ? __uint_as_float(0x7FC00000u) : ldexpf((float)r.sum[slot], e - 177);
+    if (again && h.first[slot] == (int)threadIdx.x)  // (NaN comes out above every number, one with a sign above that)
+        h.p[slot] = e >= 255 ? __uint_as_float(0x7FC00000u) : ldexpf((float)r.sum[slot], e - 177);
     __syncthreads();
 }
 

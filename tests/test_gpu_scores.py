@@ -299,6 +299,20 @@ def test_rows_of_infinities_and_nan(n, dtype):
     assert torch.isnan(loss[4]) and torch.isnan(grad[4]).all() and not torch.isnan(grad[:4]).any()
 
 
+@pytest.mark.parametrize("n,vocab", [(4, 500), (3, 60_000)])
+def test_a_teacher_of_nan(n, vocab):
+    """NaN of either sign among the entries, some of them of one token: a NaN loss, NaN in the teacher's columns."""
+    s, tok, t, w = lesson(n, vocab, 10, F32, F32, 18)
+    tok[:, 4] = tok[:, 7] = tok[:, 1]
+    for i, bad in ((1, NAN), (2, -torch.tensor(NAN))):
+        t[i, 7] = bad
+    loss, grad = tk.distill_grad(s.cuda(), tok.cuda(), t.cuda(), w.cuda())
+    assert torch.isnan(loss).cpu().tolist() == [False, True, True, False][:n]
+    listed = torch.zeros((n, vocab), dtype=torch.bool).scatter_(1, tok, True)
+    listed[[i for i in (0, 3) if i < n]] = False
+    assert torch.equal(torch.isnan(grad).cpu(), listed)
+
+
 @pytest.mark.parametrize("by", [1e-30, 1e4, 1e30])
 def test_scores_of_any_size(by):
     """Far below and above where an exponential of the scores themselves would be a number."""
