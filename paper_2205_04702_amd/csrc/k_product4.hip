@@ -22,10 +22,11 @@ constexpr int64_t CUS = 256, LDS_BYTES = 160 * 1024;
 constexpr int FP4 = 4;         // the matrix instruction's number of the format
 constexpr uint32_t GROUP = 8;  // columns of tiles that an XCD works through together
 
-// 16 bytes a lane, straight to LDS, at `at` plus the wave's `from` in a buffer; zeros past its end.
-__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t rows, uint32_t at, uint32_t from, uint8_t *dst)
+// 16 bytes a lane, straight to LDS, at `at` in a buffer; zeros past its end.  The whole place is the
+// lane's: the hardware leaves an offset that all lanes share out of its comparison with the buffer's size.
+__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t rows, uint32_t at, uint8_t *dst)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void *)dst, CHUNK, at, from, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void *)dst, CHUNK, at, 0, 0, 0);
 }
 
 // Scales of one side as the product reads them: eight bytes of a row for each step, in the caller's
@@ -85,8 +86,8 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
     const auto row_at = [](int64_t row, int64_t last) { return (uint32_t)(row < last ? row : last); };
 
     // What is loaded next: rows of a tile, a step.  The rows are buffers from the tile's first one on, whose
-    // bounds the hardware checks (strides are below 2^23, so they fit 32 bits): rows past the last are
-    // zeros, and so is everything once nothing is left to load.  Bytes behind a row's last chunk are its
+    // bounds the hardware checks (strides are below 2^23, so places in 256 rows are below 2^31): rows past the
+    // last are zeros, and so is everything once nothing is left to load.  Bytes behind a row's last chunk are its
     // neighbour's; their scales are zeros, so they count nothing (2^-254 times a finite value is below
     // anything that fp32 holds).
     uint32_t load_tile = blockIdx.x;
@@ -110,8 +111,8 @@ __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
     const auto fetch = [&](int32_t stage, int i) {  // load i, into a stage
         const bool is_x = i * NW * RPL < BM;
         const int rows = i * NW * RPL - (is_x ? 0 : BM);
-        to_lds(is_x ? x_rows : w_rows, is_x ? x_at : w_at, (uint32_t)(rows * (int)(is_x ? a.x_ld : a.w_ld) + load_step * KT),
-               sm + stage * BUF + (i * NW + wave) * RPL * KT);
+        const uint32_t from = (uint32_t)(rows * (int)(is_x ? a.x_ld : a.w_ld) + load_step * KT);
+        to_lds(is_x ? x_rows : w_rows, (is_x ? x_at : w_at) + from, sm + stage * BUF + (i * NW + wave) * RPL * KT);
     };
     const auto fetched = [&]() {  // on to the next step, or tile
         if (++load_step < end) return;
