@@ -1,0 +1,182 @@
+"""Distillation and adjusted scores in every form that their kernels take, with several different rows for each
+block, against 64 bits within the bounds that scores_reference.py derives.
+
+The number of a form's blocks at a time is 256 times the waves that it keeps on a compute unit over those of a block; a
+block goes on from row to row, so a call of more than twice as many rows makes it go on twice.  Rows without entries,
+their scores NaN, lie between the others."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+from paper_2205_04702_amd import tokens as tk  # noqa: E402
+from tests import scores_reference as one  # noqa: E402
+from tests import scores_rows_reference as ref  # noqa: E402
+from tests.rows_reference import TINY, UNIT  # noqa: E402
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+INF, NAN = math.inf, math.nan
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def lesson(n, vocab, k, dtype, teacher, seed, edges=()):
+    """Scores, tokens, the teacher's logits, weights: a third of the entries on columns around `edges` and the row's
+    ends, half of the rows with tokens that are listed twice, a tenth of the entries padding, a fifth of the rows
+    without any."""
+    g = gen(seed)
+
+    def rand(*shape):
+        return torch.rand(shape, generator=g, device="cuda")
+
+    s = (torch.randn((n, vocab), generator=g, device="cuda") * 3).to(dtype)
+    tok = torch.randint(vocab, (n, k), generator=g, device="cuda")
+    near = [v for e in (0, 16, vocab - 16, vocab - 1, *edges) for v in range(e - 9, e + 10) if 0 <= v < vocab]
+    near = torch.tensor(near, device="cuda")
+    tok = torch.where(rand(n, k) < 0.33, near[torch.randint(len(near), (n, k), generator=g, device="cuda")], tok)
+    again = tok[:, torch.randint(k, (k,), generator=g, device="cuda")]
+    tok = torch.where((rand(n, 1) < 0.5) & (rand(n, k) < 0.3), again, tok)
+    tok = torch.where(rand(n, k) < 0.1, torch.where(rand(n, k) < 0.5, -1, vocab), tok)
+    t = (torch.randn((n, k), generator=g, device="cuda") * 2).to(teacher)
+    dead = rand(n) < 0.2
+    tok[dead] = -1
+    dead = ~((tok >= 0) & (tok < vocab)).any(1)
+    s[dead] = NAN
+    return s, tok, t, rand(n) + 0.5
+
+
+def check(s, tok, t, w, T, loss, grad):
+    n, vocab = s.shape
+    step = max(1, (1 << 24) // vocab)
+    for i in range(0, n, step):
+        j = slice(i, i + step)
+        want, want_grad, loss_off, grad_off = ref.distill(s[j], tok[j], t[j], w[j], T)
+        off = (loss[j].double() - want).abs() - loss_off - want.abs() * UNIT[F32]
+        assert not torch.isnan(off).any() and off.max() <= 0, (i, off.max())
+        if grad is not None:
+            off = (grad[j].double() - want_grad).abs() - grad_off - (want_grad.abs() + grad_off) * UNIT[grad.dtype] - TINY[grad.dtype]
+            assert not torch.isnan(off).any() and off.max() <= 0, (i, off.max())
+
+
+@pytest.mark.parametrize("n,vocab,k,dtype,teacher,T", [
+    (11_000, 1021, 20, F32, F32, 1.0),     # a wave a row, 4 units a lane
+    (10_500, 203, 64, BF16, F16, 2.0),
+    (8300, 2003, 33, F32, BF16, 1.0),      # ... 16 units
+    (8300, 8181, 5, BF16, F32, 1.0),
+    (2700, 4001, 100, F32, F32, 0.5),      # 256 threads, 4 units
+    (2700, 1500, 65, F16, F32, 1.0),
+    (2100, 8300, 40, BF16, F32, 1.0),      # ... 16 units
+    (2100, 32_001, 200, BF16, BF16, 2.0),
+    (2100, 5003, 100, F32, F16, 1.0),
+    (1100, 1501, 512, BF16, F32, 1.0),     # 512 threads, 4 units
+    (1100, 8180, 300, F32, F32, 1.0),
+    (1100, 33_001, 100, BF16, F32, 1.0),   # ... 16 units
+    (1100, 65_001, 64, F16, F32, 4.0),
+    (1100, 17_001, 257, F32, F32, 1.0),
+    (520, 65_501, 64, F32, F32, 1.0),      # 1024 threads, every unit held
+    (520, 1500, 1000, BF16, F32, 1.0),
+    (520, 70_003, 300, F32, BF16, 2.0),    # ... and units past those that are held
+    (520, 140_003, 64, BF16, F32, 1.0),
+])
+def test_gradients_of_several_rows_a_block(n, vocab, k, dtype, teacher, T):
+    held = 16 * 1024 * 16 // torch.empty((), dtype=dtype).element_size()  # columns of a block of 1024 threads
+    s, tok, t, w = lesson(n, vocab, k, dtype, teacher, vocab, (held, held + 31))
+    loss, grad = tk.distill_grad(s, tok, t, w, T)
+    check(s, tok, t, w, T, loss, grad)
+    again = tk.distill_grad(s, tok, t, w, T)
+    assert torch.equal(again[0], loss) and torch.equal(again[1], grad)
+    x = s.clone()
+    again = tk.distill_grad(x, tok, t, w, T, out=x)  # in place, from rows that start alike: the same bits
+    assert again[1] is x and torch.equal(again[0], loss) and torch.equal(x, grad)
+
+
+@pytest.mark.parametrize("dtype,out", [(BF16, F32), (F32, F16), (F16, BF16)])
+@pytest.mark.parametrize("n,vocab,k", [(8300, 515, 30), (2100, 4003, 99), (1100, 8195, 270), (520, 17_003, 600)])
+def test_gradients_of_another_type(n, vocab, k, dtype, out):
+    s, tok, t, w = lesson(n, vocab, k, dtype, F32, vocab)
+    check(s, tok, t, w, 1.0, *tk.distill_grad(s, tok, t, w, dtype=out))
+
+
+@pytest.mark.parametrize("n,vocab,k,dtype,teacher,T", [
+    (300, 4000, 20, BF16, F32, 1.0),       # a wave a row, past the four units that it holds
+    (300, 12_001, 64, BF16, F32, 2.0),     # 256 threads
+    (300, 100_003, 200, BF16, BF16, 1.0),
+    (300, 5003, 256, F32, F32, 1.0),
+    (70, 70_003, 40, F32, F32, 1.0),       # 1024 threads
+    (300, 40_001, 300, F16, F16, 1.0),
+    (40, 40_001, 9, BF16, F32, 1.0),
+])
+def test_losses_past_the_held_units(n, vocab, k, dtype, teacher, T):
+    s, tok, t, w = lesson(n, vocab, k, dtype, teacher, vocab)
+    check(s, tok, t, w, T, tk.distill(s, tok, t, T), None)
+
+
+def test_losses_of_several_rows_a_block():
+    """More rows than a launch has blocks."""
+    s, tok, t, w = lesson((1 << 21) + 5000, 9, 3, BF16, F32, 1)
+    check(s, tok, t, w, 1.0, tk.distill(s, tok, t), None)
+
+
+# ------------------------------------------------------------------ adjust
+
+def request(n, vocab, length, biases, dtype, tokens, seed):
+    """Texts of any tokens, of a few that come often, and of columns where stretches begin and end."""
+    g = gen(seed)
+
+    def some(width):
+        t = torch.randint(-1, vocab + 1, (n, width), generator=g, device="cuda")
+        edge = torch.randint(vocab // 1024 + 1, (n, width), generator=g, device="cuda") * 1024
+        edge -= torch.randint(2, (n, width), generator=g, device="cuda")
+        return torch.where(torch.rand((n, width), generator=g, device="cuda") < 0.4, edge.clamp(max=vocab), t)
+
+    r = dict(scores=(torch.randn((n, vocab), generator=g, device="cuda") * 3).to(dtype), previous=None, bias_tokens=None, bias=None)
+    if length:
+        t = some(length)
+        hot = t[:, :3].gather(1, torch.randint(3, (n, length), generator=g, device="cuda")) if length >= 3 else t
+        r["previous"] = torch.where(torch.rand((n, length), generator=g, device="cuda") < 0.2, hot, t).to(tokens)
+    if biases:
+        r["bias_tokens"], r["bias"] = some(biases).to(tokens), torch.randn((n, biases), generator=g, device="cuda") * 5
+    r["penalties"] = torch.rand((n, 3), generator=g, device="cuda") + torch.tensor([0.6, -0.2, 0.0], device="cuda")
+    w = torch.randint(-2 ** 31, 2 ** 31, (n, (vocab + 31) // 32), generator=g, device="cuda")
+    w[0], w[n - 1] = -1, 0
+    r["allowed"] = w.to(torch.int32)
+    return r
+
+
+@pytest.mark.parametrize("tokens", [torch.int64, torch.int32])
+@pytest.mark.parametrize("n,vocab,length,biases,dtype", [
+    (100, 100_003, 0, 0, F32),             # a mask alone
+    (31, 100_003, 0, 0, F16),
+    (100, 100_003, 777, 20, F32),          # large calls
+    (70, 131_077, 4096, 0, F16),
+    (300, 32_768, 0, 2047, F32),
+    (2000, 5001, 300, 9, BF16),
+    (90, 100_003, 9000, 20, F32),          # ... with long texts
+    (70, 131_077, 16_384, 50, BF16),
+    (70, 131_072, 8193, 0, F16),
+    (31, 200_003, 16_384, 20, F32),        # long texts in smaller calls
+    (31, 200_003, 9001, 0, BF16),
+    (5, 262_144, 16_384, 9, F32),
+    (1, 262_144, 100_000, 9, BF16),
+    (40, 20_011, 12_345, 3, F16),
+    (3, 3001, 50_000, 3, F32),
+])
+def test_adjust_in_each_form(n, vocab, length, biases, dtype, tokens):
+    r = request(n, vocab, length, biases, dtype, tokens, vocab + length)
+    got = tk.adjust(**r)
+    want, size = ref.adjust(**r)
+    assert got.dtype == dtype and torch.equal(got == -INF, want == -INF)
+    off = torch.where(want == -INF, torch.zeros_like(want), (got.double() - want).abs()) - one.adjust_bound(want, size, dtype)
+    assert off.max() <= 0, off.max()
+    x = r["scores"].clone()
+    assert torch.equal(tk.adjust(**dict(r, scores=x), out=x), got)
