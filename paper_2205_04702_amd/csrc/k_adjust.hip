@@ -166,20 +166,46 @@ hipError_t run_adjust(const AdjustArgs &a, hipStream_t s)
             }
             return hipSuccess;
         };
-        // Large calls take longer stretches, and scores and outputs past the caches; long texts, which
-        // every stretch of a row reads, the longest (us: 512 threads of 2 units, 1024 of 2, 256 of 4,
-        // 256 of 1; then the first through the caches):
-        //   64 x 131072 bf16, 4096 tokens, 300 biases, a mask    12.2  12.4  14.0  17.0  14.2
-        //   333 x 50001 fp32, 1777 tokens                        27.8  30.7  28.6  35.7  30.9
-        //   256 x 131072 bf16, 512 tokens, 50 biases             33.1  36.7  31.0  48.3  38.9
-        //   512 x 32768 bf16, 8000 tokens                        22.5  22.6  27.3  37.0  22.6
-        //   500 x 262144 bf16, 16000 tokens, 100 biases, a mask   206   158   219   541   227
-        // Without lists, 100 x 200000 fp32 with a mask: 256 threads of 1 unit 26.2, of 4 28.8 (past the
-        // caches), 34.4 (through them).
+        // Long stretches read the lists less often, but zero and go over words that rows narrower than they are do
+        // not have.  So a row that is one short stretch (4096 bytes) takes one, and else calls take long stretches
+        // where all short ones together would read more than 2^22 tokens, or from 2^23 scores on, which then go
+        // past the caches; texts of more than 8192 tokens the longest.  Measured (us of a kernel among others, in graphs:
+        // 256 threads of 1 unit, 512 of 2, 1024 of 2, then 512 and 1024 of 2 past the caches; * what is taken):
+        //   scores, tokens each
+        //   8388 x 1000 bf16, 50                20.4*  40.7  82.9  40.5
+        //   8388 x 1000 bf16, 16384              200*   196   190   195
+        //   1677 x 5000 bf16, 1000              15.4   14.9  22.6  14.6   (just below 2^23: short ones)
+        //   3355 x 2500 fp32, 1000              24.9   22.5  36.5  21.2
+        //   8 x 131072 bf16, 4096                4.9*   5.9   7.3   5.9   7.3
+        //   8 x 131072 bf16, 8192                6.0*   6.6   7.7   6.6   7.7
+        //   8 x 131072 bf16, 16384               8.4    7.8*  8.7   7.8   8.6
+        //   16 x 131072 bf16, 300                5.1*   5.3   6.1   5.3   6.1
+        //   16 x 131072 bf16, 4096               6.4*   6.1   7.5   6.1   7.5
+        //   32 x 131072 bf16, 300                7.7*   7.4   7.0   6.9   6.7
+        //   32 x 131072 bf16, 4096               9.5    8.5*  8.4   7.7   7.8
+        //   32 x 131072 bf16, 16384             21.0   11.9  10.3* 10.4   9.0
+        //   31 x 262144 fp32, 300               16.4*  14.0  15.7  15.1  16.4
+        //   31 x 262144 fp32, 4096              22.5   14.7* 16.3  16.2  17.2
+        //   31 x 262144 fp32, 16384             62.8   24.6  19.8* 26.3  20.4
+        //   64 x 131072 bf16, 300               11.4   11.2  11.3   9.0*  8.8
+        //   64 x 131072 bf16, 4096              15.4   13.0  13.6  10.9* 11.0
+        //   64 x 131072 bf16, 8192              21.6   15.4  14.3  12.8* 11.6
+        //   64 x 131072 bf16, 16384             36.0   18.4  15.8  17.2  14.6*
+        //   200 x 50001 fp32, 300               23.3   19.6  21.3  18.6* 20.6
+        //   512 x 32768 bf16, 16384             81.4   38.0  34.8  31.1  28.5*
+        // What reads the scores next finds those that went past the caches in memory only: with a maximum of each row
+        // behind the call, 32 x 131072 of 300 tokens takes 34.2 through the caches and 44.6 past them, 64 x 131072
+        // 38.0 and 48.0.
+        // Without lists, a mask alone (256 threads of 1 unit through the caches and past them): 32 x 131072 bf16 4.6
+        // and 4.1, 64 x 131072 6.9 and 6.9, 128 x 131072 11.2 and 12.0; 100 x 200000 fp32 26.2 past them.
         const bool large = a.n * a.vocab >= 1 << 23;
         if (!a.previous && !a.bias_tokens)
             return large ? go(k_adjust<T, 256, 1, false, true>, 256, 1) : go(k_adjust<T, 256, 1, false, false>, 256, 1);
-        if (!large) return go(k_adjust<T, 256, 1, true, false>, 256, 1);
+        const int64_t tokens = (a.previous ? a.length : 0) + (a.bias_tokens ? a.biases : 0);
+        const int64_t stretches = (a.vocab + 256 * COLS<T> - 1) / (256 * COLS<T>), reads = a.n * stretches * tokens;
+        if (stretches == 1 || (!large && reads <= 1 << 22)) return go(k_adjust<T, 256, 1, true, false>, 256, 1);
+        if (!large)
+            return a.length > 8192 && reads >= 1 << 24 ? go(k_adjust<T, 1024, 2, true, false>, 1024, 2) : go(k_adjust<T, 512, 2, true, false>, 512, 2);
         return a.length > 8192 ? go(k_adjust<T, 1024, 2, true, true>, 1024, 2) : go(k_adjust<T, 512, 2, true, true>, 512, 2);
     });
 }

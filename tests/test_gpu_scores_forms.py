@@ -164,7 +164,10 @@ def request(n, vocab, length, biases, dtype, tokens, seed):
     (90, 100_003, 9000, 20, F32),          # ... with long texts
     (70, 131_077, 16_384, 50, BF16),
     (70, 131_072, 8193, 0, F16),
-    (31, 200_003, 16_384, 20, F32),        # long texts in smaller calls
+    (9000, 1000, 77, 5, BF16),             # ... of rows that are one short stretch
+    (9000, 1021, 9, 0, F32),
+    (31, 100_003, 4096, 0, F32),           # smaller calls whose short stretches would read much
+    (31, 200_003, 16_384, 20, F32),        # ... and with long texts
     (31, 200_003, 9001, 0, BF16),
     (5, 262_144, 16_384, 9, F32),
     (1, 262_144, 100_000, 9, BF16),
