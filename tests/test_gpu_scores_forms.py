@@ -183,3 +183,65 @@ def test_adjust_in_each_form(n, vocab, length, biases, dtype, tokens):
     assert off.max() <= 0, off.max()
     x = r["scores"].clone()
     assert torch.equal(tk.adjust(**dict(r, scores=x), out=x), got)
+
+
+def test_adjust_of_more_rows_than_one_launch_has_blocks():
+    """Blocks of 1024 threads, 2^21 to a launch."""
+    n, vocab = (1 << 21) + 3, 2049
+    s = torch.zeros((n, vocab), dtype=BF16, device="cuda")
+    s[:, 2048] = 2.0
+    previous = torch.cat([torch.full((3,), 2048), torch.full((8200,), -1)]).cuda()  # for all rows
+    got = tk.adjust(s, previous, 2.0, 0.25, 0.125, out=s)
+    assert (got[:, 2048] == 2.0 / 2 - 0.25 - 3 * 0.125).all()
+    got[:, 2048] = 0
+    assert not got.any()
+
+
+# ------------------------------------------------------------------ captured
+
+def large_calls(seed):
+    """The operators in the forms that large calls take, those of several launches among them: the tensors that they
+    read, and the calls."""
+    g = gen(seed)
+
+    def randn(*shape, dtype=F32):
+        return torch.randn(shape, generator=g, device="cuda").to(dtype)
+
+    inputs, calls = [], []
+    for n, vocab, k, dtype in ((1100, 8300, 40, BF16), (600, 17_001, 100, F32), (300, 131_077, 64, BF16), (2700, 1500, 100, F16), (64, 60_001, 300, F32)):
+        s, t = randn(n, vocab, dtype=dtype), randn(n, k)
+        tok = torch.randint(-1, vocab, (n, k), generator=g, device="cuda")
+        inputs += [s, t]
+        calls += [lambda s=s, t=t, tok=tok: tk.distill_grad(s, tok, t, 0.5, 2.0), lambda s=s, t=t, tok=tok: [tk.distill(s, tok, t)]]
+    for n, vocab, length, dtype in ((70, 131_077, 777, BF16), (90, 100_003, 9000, F32), (31, 100_003, 9000, F32), (31, 100_003, 4096, F16), (9000, 1000, 50, BF16)):
+        s, previous = randn(n, vocab, dtype=dtype), torch.randint(-1, vocab, (n, length), generator=g, device="cuda")
+        inputs.append(s)
+        calls.append(lambda s=s, previous=previous: [tk.adjust(s, previous, 1.2, 0.5, 0.25)])
+    x, w, at = randn(4000, 4000, dtype=BF16), randn(16, 4000), torch.randint(4000, (9000,), generator=g, device="cuda")
+    inputs += [x, w]
+
+    def rows():
+        big, few = tk.quantize4(x), tk.quantize4(w)
+        return [*big, *few, tk.product4(*big, *big), tk.product4(*few, *few), *(tk.cache_read4(*big, at, 4000, dtype) for dtype in (BF16, F16, F32))]
+
+    return inputs, lambda: [y for call in (*calls, rows) for y in call()]
+
+
+def test_captured_and_replayed_in_large_forms():
+    graphs = []
+    for seed in (1, 2):
+        inputs, go = large_calls(seed)
+        go()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = go()
+        graphs.append((inputs, go, graph, outs))
+    for turn in range(3):
+        for inputs, go, graph, outs in graphs:
+            for t in inputs:
+                t.mul_(-0.75).add_(0.01 * turn)
+            graph.replay()
+            torch.cuda.synchronize()
+            for i, (got, want) in enumerate(zip(outs, go())):
+                assert torch.equal(got, want), (turn, i)
