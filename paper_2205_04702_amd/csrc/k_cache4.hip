@@ -148,7 +148,7 @@ struct Cache4Read {
 // in a store of their own (65536 random rows of 1024 74 us, so 43).  A thread's columns end where 16
 // aligned bytes of the output do, and each four threads' where 64 do, wherever the row starts, which lets stores go past the caches (LEAD:
 // columns that its first threads lack): parts of 64 bytes that two waves write past them cost a read each
-// (rows of 1001 85 us through the caches, 47 so).
+// (rows of 1001 85 us through the caches, 47 so, and 60 to 71 right behind a write of as many rows).
 template <typename IX, bool LEAD>
 struct Cache4ReadQuads {
     Cache4Args a;

@@ -237,9 +237,11 @@ __device__ __forceinline__ Soft wave_soft(Soft s, float c)
 // hash from token to entry, so that a unit is stored once, with its corrections (stored over
 // the gradient afterwards, they cost 58 of 181 us at 20000 x 8192 in bf16 with 64 entries).
 //
-// Bound by the bytes: 4096 x 131072 in bf16 385 to 420 us (5.1 to 5.6 TB/s; 2 % less with an exponent of one
+// Bound by the bytes: 4096 x 131072 in bf16 385 to 424 us (5.1 to 5.6 TB/s; 2 % less with an exponent of one
 // operation, 7 % without exponentials), the loss alone of 2048 x 131072 87 us (6.2 TB/s).  Read
-// again and not held, 4096 x 131072 took 596 us (of 507 at the time).
+// again and not held, 4096 x 131072 took 596 us (of 507 at the time).  Four waves a SIMD leave 128 registers a
+// thread: with 16 units held up to 6 of a thread's numbers that no row changes are in memory, and loaded once a
+// row where they are needed (15 to 19 scalars lie in lanes of vector registers); the units stay.
 //
 // Units are counted from where 64 aligned bytes of the gradient's row start, and the columns before (head) and
 // behind them (rest) go one by one, so that the gradient may go past the caches wherever rows start: parts

@@ -51,10 +51,11 @@ struct Scales4 {
 // those of its half, a byte for each set.  w is the left factor of the matrix instruction: its four
 // consecutive rows per lane are four consecutive outputs.
 //
-// 8192^3 272 us, 4.0 PFLOP/s, 8192 x 16384 x 4096 302; matrix instructions alone, on registers of random
-// codes, reach 6.1 PFLOP/s at the clock that power leaves (8.7 on zeros).  256 x 256 in four waves of
+// 8192^3 270 us, 4.1 PFLOP/s, 8192 x 16384 x 4096 302; matrix instructions alone, on registers of random
+// codes, reach 6.1 PFLOP/s at the clock that power leaves (8.7 on zeros).  Left out, the scales' loads are 10 and
+// 16 us of that, the outputs 16 and 32, the rows' loads 104 and 79, all three 121 and 134.  256 x 256 in four waves of
 // 128 x 128 and not eight of 128 x 64: with those LDS was read for as long as the matrix cores were
-// busy (517 us with steps of 64 bytes and the scales through LDS; without scales 326, without loads 328).
+// busy (8192^3 513 us with steps of 64 bytes and the scales through LDS; without scales 326, without loads 328).
 template <int BM, int BN, int WM, int WN, int STAGES, typename TO, bool PARTIAL>
 __global__ void __launch_bounds__(BM / WM *BN / WN *WAVE)
     k_product4(Product4Args a, Scales4 sx, Scales4 sw, int32_t tiles_n, uint32_t tiles_m, int32_t per_split)
@@ -402,19 +403,24 @@ static int64_t steps_of(int32_t blocks) { return (blocks + CPR - 1) / CPR; }
 // what a CU has to do one after the other: rounds of as many blocks as run at a time, each a fixed time
 // (first loads, outputs) and its steps of k, with a block on a CU or as many as fit; for tiles of 256
 // the packing of the scales; for parts a second launch and their traffic.  Measured on both sides
-// of the lines that it draws (us a call, of which 8.7 are the host's, in two launches 13; bf16):
+// of the lines that it draws (us of the kernels among others, in graphs; a call outside of one takes the host 9,
+// of two launches 13; bf16; * what is taken).  Where bytes bind (1, 16 and 64 rows against 131072) the times are
+// up to twice the estimate, in the small tiles alike:
 //                          256x256  128x128  64x128  64x64  32x64   in parts
-//   8192 x 16384 x 4096        302
-//   8192 x 8192 x 512           52       48      61     73     93
-//   4000 x 4000 x 4000          44       57      74     94    107
-//   4000 x 4000 x 1000          24       18      22     28     34
-//   777 x 10001 x 1000          32       18      17     19     21
-//   2048 x 2048 x 2048          26       11      12     14     18
-//   256 x 8192 x 8192           55       29      23     28     36   26 (2 of 128x128)
-//   128 x 8192 x 8192           54       29      22     18     19   19 (2 of 64x128)
-//   64 x 4096 x 4096            33       13      11      9      9   13 (2 of any)
-//   1 x 131072 x 2048           53       31      28     29     28   37 (2 of 64x128)
-//   1 x 4096 x 8192             53       22      19     16     15   13 (4 of 64x64)
+//   8192 x 16384 x 4096       300*     451
+//   8192 x 8192 x 512          50       48*     62     74     91
+//   4000 x 4000 x 4000         44*      55      75     95    110
+//   4000 x 4000 x 1000         23       17*     21     29     34
+//   777 x 10001 x 1000         33       18      18*    20     21
+//   2048 x 2048 x 2048         26       11*     12     15     18    26 (2 of 128x128)
+//   256 x 8192 x 8192          57       29      23*    28     36    26 (2 of 128x128)
+//   128 x 8192 x 8192          55       29      23     18*    19    19 (2 of 64x128)
+//   64 x 8192 x 8192           55       25      23     18     16*   15 (2 of 64x64, 4 of 64x128)
+//   64 x 131072 x 4096         86       76      74*    90    106
+//   16 x 131072 x 4096         80       65      62     71     61*
+//   64 x 4096 x 4096           33       14      12     10      9*   10 (2 of 64x64 or 32x64)
+//   1 x 131072 x 2048          51       31      29     29     28*
+//   1 x 4096 x 8192            54       23      20     16     15    10* (8 of 32x64; 4 of 32x64 9, of 64x64 10)
 struct Cut {
     int32_t tile, splits;
 };
@@ -442,7 +448,8 @@ static Cut cut_product4(int64_t m, int64_t n, int32_t blocks)
 }
 
 // The scales of tiles of 256 are packed: what each reads of them in the caller's rows is as many lines as
-// the factors' (8192^3: 324 us with both in the caller's rows, 272 packed, of which 5 for packing).
+// the factors' (8192^3: 324 us with both in the caller's rows, 272 packed, when it was brought in; the packing of
+// 8192 and 16384 rows of 4096 columns takes 4 and 6).
 // (In one launch: of fewer than 2^30 rows.)
 static bool packs(int64_t m, int64_t n, const Cut &c) { return c.tile == 0 && m < 1 << 30 && n < 1 << 30; }
 
